@@ -53,6 +53,7 @@ extern "C" {
 #define SPECATTN_ROW_OVERFLOW 2     /* the list has more entries than idx_stride; truncated */
 #define SPECATTN_ROW_BAD_INDEX 4    /* verify met a position or page id out of range */
 #define SPECATTN_ROW_TIMEOUT 8      /* a bounded device-side wait ran out; outputs invalid */
+#define SPECATTN_ROW_INVALID_VALUE 16 /* a K/V row held NaN or an infinity, or spans more than binary32 */
 
 /* ---- limits ---------------------------------------------------------------------------- */
 #define SPECATTN_MAX_DRAFT_LAYERS 64
@@ -408,6 +409,241 @@ typedef struct specattn_step_host_args {
 } specattn_step_host_args;
 
 int specattn_verify_step_host(const specattn_step_host_args* args, void* cuda_stream);
+
+/* ========================================================================================
+ * A K/V cache held in 4 bits.
+ *
+ * (No counterpart in the paper, whose cache is 16 bits wide; the operations below serve the same
+ * step from a cache of 68 instead of 256 bytes a row.)
+ *
+ * A row is the 128 values x of one position, KV head and side (kv = 0 keys, 1 values).  It is
+ * stored as a scale s and a zero point z in the 16-bit type of the model and a 4-bit code per value:
+ *     z = min x      s = (max x - z) / 15, the quotient rounded to binary32, then to 16 bits
+ *     c_e = min(15, rint((x_e - z) / s))       (difference and quotient rounded to binary32,
+ *                                              rint to even; all codes 0 where s < 2^-126)
+ * and stands for s c_e + z.  z is exact, being one of the values; s below 2^-126 is stored as 0.  A
+ * row that holds NaN or an infinity, or whose max x - min x overflows binary32, is stored as s = z =
+ * NaN, c = 0.
+ *   codes:  byte e/2 of a row holds code e in its low and code e + 1 in its high four bits (e even).
+ *           Row (page, kv, slot, head) starts at codes + page*stride_page + kv*stride_kv +
+ *           slot*stride_slot + head*stride_head (bytes; base 16-byte aligned, strides multiples of 16).
+ *   params: s and z, side by side, at params + page*pstride_page + ... (16-bit elements; base
+ *           4-byte aligned, strides even).
+ * Position i of sequence b lives in page block_table[b * block_table_stride + i / page_size] at slot
+ * i % page_size; with block_table == NULL that page is b * block_table_stride + i / page_size.  Unlike
+ * the 16-bit pool's, n_pages is required: page ids outside [0, n_pages) are never followed.
+ * A layout with the slots of one page and head side by side (stride_slot = 64, stride_head =
+ * page_size * 64, and alike for params) lets a scan of everything read whole 32-byte sectors of params.
+ * ======================================================================================== */
+#define SPECATTN_DTYPE_BF16 0
+#define SPECATTN_DTYPE_FP16 1
+
+typedef struct specattn_kv4_cache {
+  void* codes;
+  void* params;
+  int64_t n_pages;
+  int64_t stride_page, stride_kv, stride_slot, stride_head;
+  int64_t pstride_page, pstride_kv, pstride_slot, pstride_head;
+  const int32_t* block_table;
+  int64_t block_table_stride;
+  int32_t page_size;
+  int32_t dtype; /* SPECATTN_DTYPE_*: of params, and of the rows that come in or go out */
+} specattn_kv4_cache;
+
+/* specattn_kv4_append -- writes new K/V rows: row t < n_new[b] of sequence b goes to position
+ * start[b] + t.  Everything from one token per sequence to whole prompts.
+ * specattn_kv4_read   -- the reverse: rows start[b] + t, t < n_new[b], as 16-bit values
+ * (s c + z in binary32, rounded to even).  Rows t >= n_new[b] of the buffers are neither read nor
+ * written by either.
+ * k, v: element (b, t, head, e) at b*stride_batch + t*stride_token + head*stride_head + e, 16-byte
+ * aligned, strides multiples of 8.  n_new == NULL: n_tokens of every sequence (values beyond
+ * [0, n_tokens] are clamped).  status (int32 [batch], optional) is cleared by the call and receives
+ * SPECATTN_ROW_BAD_INDEX where a position is negative or beyond the block table or its page id out of range
+ * (that row is skipped) and, on append, SPECATTN_ROW_INVALID_VALUE.  head_dim == 128. */
+typedef struct specattn_kv4_rows_args {
+  uint32_t struct_size;
+  int32_t batch;
+  int32_t n_tokens;
+  int32_t n_kv_heads;
+  int32_t head_dim;
+  int32_t reserved; /* 0 */
+  specattn_kv4_cache cache;
+  void* k;
+  void* v;
+  int64_t k_stride_batch, k_stride_token, k_stride_head;
+  int64_t v_stride_batch, v_stride_token, v_stride_head;
+  const int32_t* start; /* [batch] */
+  const int32_t* n_new; /* [batch] or NULL */
+  int32_t* status;      /* [batch] or NULL */
+} specattn_kv4_rows_args;
+
+int specattn_kv4_append(const specattn_kv4_rows_args* args, void* cuda_stream);
+int specattn_kv4_read(const specattn_kv4_rows_args* args, void* cuda_stream);
+
+/* specattn_kv4_verify -- specattn_sparse_verify over a cache held in 4 bits.
+ *
+ * The same operation on the values that the codes stand for: for query row q of KV head hk and the
+ * positions i of its list (then the in-flight tail),
+ *   s_i = sm_scale * (s_K[i] * sum_e q_e c_K[i,e] + z_K[i] * sum_e q_e)
+ *   out_e = sum_i p_i (s_V[i] c_V[i,e] + z_V[i]) / sum_i p_i,  p_i = exp(s_i - max s),
+ *   lse   = max s + ln sum_i p_i.
+ * An empty list gives out = 0, lse = -inf.  Lists, dense, kv_len, tail_len, sm_scale and n_groups as
+ * in specattn_sparse_verify; one query and no list (n_q = 1, dense = 1) is plain decoding.  Scores,
+ * sums and outputs are binary32; the weights p_i enter the second product in 11 bits.
+ * q is of the cache's dtype, [batch, n_q, n_q_heads, 128], 16-byte aligned; out has the same shape, in
+ * that dtype or (out_f32 != 0) binary32, 16-byte aligned; lse binary32 [batch, n_q, n_q_heads].
+ * status (int32 [batch], optional) is written by the call: SPECATTN_ROW_BAD_INDEX where a listed
+ * position is outside [0, kv_len[b]), a position beyond the block table or its page id out of range
+ * (such entries are read from position 0 / page 0 instead), else 0.
+ * Positions whose row holds NaN make the rows that attend them NaN; rows that no list names, masked tail rows
+ * and the rest of the last page are not looked at.
+ * Requirements: head_dim == 128; n_q * (n_q_heads / n_kv_heads) <= 64; batch * n_kv_heads <= 2048; lists
+ * and, where dense, block_table_stride * page_size of at most 2^23 positions.
+ * workspace: specattn_kv4_verify_workspace_bytes() bytes, 256-byte aligned, no preparation and no
+ * state between calls; two calls that may overlap on the GPU need separate ones.
+ * (The call signals programmatic launch completion early: it does not count as the launch in front of a
+ * specattn_sparse_verify call with SPECATTN_VERIFY_LISTS_STABLE.) */
+typedef struct specattn_kv4_verify_args {
+  uint32_t struct_size;
+  int32_t batch;
+  int32_t n_q;
+  int32_t n_q_heads;
+  int32_t n_kv_heads;
+  int32_t head_dim;
+  int32_t n_groups;
+  int32_t dense;
+  specattn_kv4_cache cache;
+  const void* q;
+  const int32_t* kv_len; /* [batch] */
+  const int32_t* idx;    /* [batch, n_groups, idx_stride] */
+  int64_t idx_stride;
+  const int32_t* counts; /* [batch, n_groups] */
+  float sm_scale;        /* > 0, or 0 => 1/sqrt(head_dim); negative or NaN is rejected */
+  int32_t out_f32;
+  void* out;
+  float* lse;
+  int32_t* status; /* [batch] or NULL */
+  void* workspace;
+  size_t workspace_bytes;
+  int32_t tail_len; /* 0 <= tail_len <= 64 */
+  int32_t reserved; /* 0 */
+} specattn_kv4_verify_args;
+
+/* Bytes of workspace for these shapes on the current device (0 on argument error). */
+size_t specattn_kv4_verify_workspace_bytes(const specattn_kv4_verify_args* args);
+int specattn_kv4_verify(const specattn_kv4_verify_args* args, void* cuda_stream);
+
+/* ========================================================================================
+ * Eviction by accumulated attention weight.
+ *
+ * (Not in the paper, which keeps every row and skips most of them per step.  The draft model's
+ * attention maps, which selection reads anyway, say which rows have not been attended for long.)
+ *
+ * specattn_accumulate: for every draft layer u with draft_probs[u] != NULL, sequence b, group g
+ *   scores_out[u,b,g,i] = decay * scores_in[u,b,g,i] + sum over heads h feeding g and s < gamma of
+ *                         draft_probs[u][b,h,s,i],       i < min(kv_len[b], L_stride, score_stride)
+ * with the sum in binary64, rounded once.  scores_in == NULL counts as zeros and may equal
+ * scores_out.  Other entries are left as they were.  Where a contributing probability is negative,
+ * NaN or infinite the position gets its old value, undecayed, and row_status[u,b,g] (optional, cleared by
+ * the call, for every u) SPECATTN_ROW_INVALID_PROB.
+ * Arrays, limits and alignment of draft_probs, kv_len and head_group as in specattn_select_topp;
+ * scores are binary32 [n_layers, batch, n_groups, score_stride]. */
+typedef struct specattn_accumulate_args {
+  uint32_t struct_size;
+  int32_t n_layers;
+  int32_t batch;
+  int32_t n_draft_heads;
+  int32_t gamma;
+  int32_t n_groups;
+  int64_t L_stride;
+  const float* const* draft_probs; /* HOST array [n_layers] of device pointers or NULL */
+  const int32_t* kv_len;           /* [batch] */
+  const int32_t* head_group;       /* HOST [n_draft_heads] or NULL */
+  double decay;                    /* finite, >= 0 */
+  const float* scores_in;
+  float* scores_out;
+  int64_t score_stride;
+  int32_t* row_status; /* [n_layers, batch, n_groups] or NULL */
+} specattn_accumulate_args;
+
+int specattn_accumulate(const specattn_accumulate_args* args, void* cuda_stream);
+
+/* specattn_evict: which rows stay when every sequence gives up all but `budget` of its positions, and
+ * which moves close the gaps.  For each list (u, b, g), n = kv_len[b] (clamped to [0, L]):
+ *   slot i < n holds token pos(i) = positions[u,b,g,i], or i where positions == NULL; the sequence has
+ *   seen seq_len[b] tokens (n where seq_len == NULL).  A slot is protected when pos(i) < n_sink or
+ *   pos(i) >= seq_len[b] - n_recent.  The m = min(n, budget) slots that stay are the protected ones, then
+ *   those of the highest score; among equals the lower slot stays.  (-0 counts as 0, NaN as -inf.)
+ *   Moves: the slots >= m that stay, ascending, go to the slots < m that do not, ascending:
+ *   src[u,b,g,j] -> dst[u,b,g,j], j < n_moves[u,b,g] <= min(budget, L - budget).  Entries behind are
+ *   left as they were.  No slot is both read and written, so moves may run in any order; rows in front
+ *   that stay are not touched, and slots stop being in token order: positions tells it.
+ *   new_len[b] = m, which is the sequence's kv_len once the rows have been moved.
+ *   scores_out (optional): the scores after the moves, 0 in slots [m, n) so that tokens appended there
+ *   start from nothing; may equal scores.  positions_out (optional, needs positions): likewise, slots
+ *   >= m left as they were; may equal positions.
+ * All of scores, positions, scores_out and positions_out are [n_layers, batch, n_groups, L].
+ * Requirements: 1 <= L <= SPECATTN_MAX_KV_LEN; budget >= 1; n_sink, n_recent >= 0, their sum <= budget;
+ * move_stride >= min(budget, L - budget); new_len must not be kv_len or seq_len. */
+typedef struct specattn_evict_args {
+  uint32_t struct_size;
+  int32_t n_layers;
+  int32_t batch;
+  int32_t n_groups;
+  int64_t L;
+  const float* scores;
+  const int32_t* kv_len; /* [batch] */
+  int32_t budget;
+  int32_t n_sink;
+  int32_t n_recent;
+  int32_t reserved;         /* 0 */
+  const int32_t* positions; /* or NULL */
+  const int32_t* seq_len;   /* [batch] or NULL */
+  int32_t* src;             /* [n_layers, batch, n_groups, move_stride] */
+  int32_t* dst;
+  int64_t move_stride;
+  int32_t* n_moves; /* [n_layers, batch, n_groups] */
+  int32_t* new_len; /* [batch] */
+  float* scores_out;
+  int32_t* positions_out;
+} specattn_evict_args;
+
+int specattn_evict(const specattn_evict_args* args, void* cuda_stream);
+
+/* specattn_move_rows: carries out the moves of ONE draft layer's lists in the pools of the target
+ * layers that follow it, one launch for up to 32 of them: for every pool, sequence b, move j < n_moves[b,g]
+ * and KV head of group g (n_groups == 1: all heads; n_groups == n_kv_heads: head g), K and V:
+ *   row(dst[b,g,j]) = row(src[b,g,j]).
+ * A pool is any array of rows of row_bytes (a multiple of 16) addressed (page, kv, slot, head) by strides
+ * in BYTES (multiples of 16; base 16-byte aligned): the bf16 pools of specattn_sparse_verify (256) or
+ * the codes of a 4-bit cache (64); params, where set, are rows of param_bytes (a multiple of 4) beside
+ * them, 4-byte aligned.  No position may be both a source and a destination of a list, nor twice a destination.
+ * status (int32 [batch], optional) is cleared by the call and receives SPECATTN_ROW_BAD_INDEX where a
+ * position is negative or beyond the block table, or its page id outside [0, n_pages) (the move is skipped). */
+typedef struct specattn_move_args {
+  uint32_t struct_size;
+  int32_t n_pools;
+  int32_t batch;
+  int32_t n_groups;
+  int32_t n_kv_heads;
+  int32_t page_size;
+  int64_t n_pages;
+  void* const* pools; /* HOST [n_pools] */
+  int64_t row_bytes;
+  int64_t stride_page, stride_kv, stride_slot, stride_head;
+  void* const* params; /* HOST [n_pools] or NULL */
+  int64_t param_bytes;
+  int64_t pstride_page, pstride_kv, pstride_slot, pstride_head;
+  const int32_t* block_table; /* [batch, block_table_stride], or NULL: contiguous, as in verify */
+  int64_t block_table_stride;
+  const int32_t* src; /* [batch, n_groups, move_stride] */
+  const int32_t* dst;
+  int64_t move_stride;
+  const int32_t* n_moves; /* [batch, n_groups] */
+  int32_t* status;        /* [batch] or NULL */
+} specattn_move_args;
+
+int specattn_move_rows(const specattn_move_args* args, void* cuda_stream);
 
 /* Text for a SPECATTN_ERR_* return code (static storage, never NULL). */
 const char* specattn_status_string(int code);

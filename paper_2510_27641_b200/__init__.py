@@ -20,9 +20,11 @@ __all__ = ["select_topp", "sparse_verify", "sparse_verify_static", "verify_works
            "VERIFY_LISTS_STABLE", "VERIFY_ENGINE_MMA_SYNC", "VERIFY_ENGINE_TCGEN05",
            "VERIFY_TEST_LOSE_ARRIVAL", "VERIFY_PAGE_LISTS", "VERIFY_INIT_WORKSPACE", "VERIFY_INIT_STATUS", "SELECT_FORM_AUTO", "SELECT_FORM_CLUSTER",
            "SELECT_FORM_TWO_LAUNCH", "verify_plan",
-           "verify_plan_buffer", "verify_plan_many"]
+           "verify_plan_buffer", "verify_plan_many", "ROW_INVALID_VALUE", "kv4_cache", "kv4_append", "kv4_read", "kv4_verify",
+           "kv4_verify_workspace_bytes", "accumulate_attention", "evict", "move_rows", "Kv4Cache", "Kv4RowsArgs", "Kv4VerifyArgs",
+           "AccumulateArgs", "EvictArgs", "MoveArgs"]
 
-ROW_OK, ROW_INVALID_PROB, ROW_OVERFLOW, ROW_BAD_INDEX, ROW_TIMEOUT = 0, 1, 2, 4, 8
+ROW_OK, ROW_INVALID_PROB, ROW_OVERFLOW, ROW_BAD_INDEX, ROW_TIMEOUT, ROW_INVALID_VALUE = 0, 1, 2, 4, 8, 16
 VERIFY_LISTS_STABLE = 1
 VERIFY_ENGINE_MMA_SYNC = 2
 VERIFY_ENGINE_TCGEN05 = 4
@@ -67,6 +69,63 @@ class VerifyArgs(C.Structure):
                 ("tail_len", C.c_int32), ("plan", C.c_void_p)]
 
 
+class Kv4Cache(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("params", C.c_void_p), ("n_pages", C.c_int64),
+                ("stride_page", C.c_int64), ("stride_kv", C.c_int64), ("stride_slot", C.c_int64),
+                ("stride_head", C.c_int64), ("pstride_page", C.c_int64), ("pstride_kv", C.c_int64),
+                ("pstride_slot", C.c_int64), ("pstride_head", C.c_int64), ("block_table", C.c_void_p),
+                ("block_table_stride", C.c_int64), ("page_size", C.c_int32), ("dtype", C.c_int32)]
+
+
+class Kv4RowsArgs(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("batch", C.c_int32), ("n_tokens", C.c_int32),
+                ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("reserved", C.c_int32),
+                ("cache", Kv4Cache), ("k", C.c_void_p), ("v", C.c_void_p),
+                ("k_stride_batch", C.c_int64), ("k_stride_token", C.c_int64), ("k_stride_head", C.c_int64),
+                ("v_stride_batch", C.c_int64), ("v_stride_token", C.c_int64), ("v_stride_head", C.c_int64),
+                ("start", C.c_void_p), ("n_new", C.c_void_p), ("status", C.c_void_p)]
+
+
+class Kv4VerifyArgs(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("batch", C.c_int32), ("n_q", C.c_int32),
+                ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("n_groups", C.c_int32), ("dense", C.c_int32), ("cache", Kv4Cache), ("q", C.c_void_p),
+                ("kv_len", C.c_void_p), ("idx", C.c_void_p), ("idx_stride", C.c_int64),
+                ("counts", C.c_void_p), ("sm_scale", C.c_float), ("out_f32", C.c_int32),
+                ("out", C.c_void_p), ("lse", C.c_void_p), ("status", C.c_void_p),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t), ("tail_len", C.c_int32),
+                ("reserved", C.c_int32)]
+
+
+class AccumulateArgs(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("n_layers", C.c_int32), ("batch", C.c_int32),
+                ("n_draft_heads", C.c_int32), ("gamma", C.c_int32), ("n_groups", C.c_int32),
+                ("L_stride", C.c_int64), ("draft_probs", C.POINTER(C.c_void_p)), ("kv_len", C.c_void_p),
+                ("head_group", C.POINTER(C.c_int32)), ("decay", C.c_double), ("scores_in", C.c_void_p),
+                ("scores_out", C.c_void_p), ("score_stride", C.c_int64), ("row_status", C.c_void_p)]
+
+
+class EvictArgs(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("n_layers", C.c_int32), ("batch", C.c_int32),
+                ("n_groups", C.c_int32), ("L", C.c_int64), ("scores", C.c_void_p), ("kv_len", C.c_void_p),
+                ("budget", C.c_int32), ("n_sink", C.c_int32), ("n_recent", C.c_int32), ("reserved", C.c_int32),
+                ("positions", C.c_void_p), ("seq_len", C.c_void_p), ("src", C.c_void_p), ("dst", C.c_void_p),
+                ("move_stride", C.c_int64), ("n_moves", C.c_void_p), ("new_len", C.c_void_p),
+                ("scores_out", C.c_void_p), ("positions_out", C.c_void_p)]
+
+
+class MoveArgs(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("n_pools", C.c_int32), ("batch", C.c_int32),
+                ("n_groups", C.c_int32), ("n_kv_heads", C.c_int32), ("page_size", C.c_int32),
+                ("n_pages", C.c_int64), ("pools", C.POINTER(C.c_void_p)), ("row_bytes", C.c_int64),
+                ("stride_page", C.c_int64), ("stride_kv", C.c_int64), ("stride_slot", C.c_int64),
+                ("stride_head", C.c_int64), ("params", C.POINTER(C.c_void_p)), ("param_bytes", C.c_int64),
+                ("pstride_page", C.c_int64), ("pstride_kv", C.c_int64), ("pstride_slot", C.c_int64),
+                ("pstride_head", C.c_int64), ("block_table", C.c_void_p), ("block_table_stride", C.c_int64),
+                ("src", C.c_void_p), ("dst", C.c_void_p), ("move_stride", C.c_int64),
+                ("n_moves", C.c_void_p), ("status", C.c_void_p)]
+
+
 class StepHostArgs(C.Structure):
     _fields_ = [("struct_size", C.c_uint32), ("n_target_layers", C.c_int32),
                 ("select", C.POINTER(SelectArgs)), ("draft_probs_host", C.POINTER(C.c_void_p)),
@@ -107,6 +166,12 @@ def lib() -> C.CDLL:
         L.specattn_sparse_verify_static.restype = C.c_int
         L.specattn_verify_step_host.argtypes = [C.POINTER(StepHostArgs), C.c_void_p]
         L.specattn_verify_step_host.restype = C.c_int
+        L.specattn_kv4_verify_workspace_bytes.argtypes = [C.POINTER(Kv4VerifyArgs)]
+        L.specattn_kv4_verify_workspace_bytes.restype = C.c_size_t
+        for name, args in (("kv4_append", Kv4RowsArgs), ("kv4_read", Kv4RowsArgs), ("kv4_verify", Kv4VerifyArgs),
+                           ("accumulate", AccumulateArgs), ("evict", EvictArgs), ("move_rows", MoveArgs)):
+            entry = getattr(L, "specattn_" + name)
+            entry.argtypes, entry.restype = [C.POINTER(args), C.c_void_p], C.c_int
         L.specattn_status_string.argtypes = [C.c_int]
         L.specattn_status_string.restype = C.c_char_p
         L.specattn_kernel_launch_count.argtypes = []
@@ -465,3 +530,7 @@ def verify_step_host(select_args: SelectArgs, draft_probs_host: Sequence[torch.T
     rc = lib().specattn_verify_step_host(C.byref(a), _stream_ptr(stream))
     if rc != 0:
         raise SpecAttnError(rc, "specattn_verify_step_host")
+
+
+from .cache_ops import (accumulate_attention, evict, kv4_append, kv4_cache, kv4_read, kv4_verify,  # noqa: E402
+                        kv4_verify_workspace_bytes, move_rows)

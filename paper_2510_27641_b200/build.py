@@ -14,7 +14,7 @@ CSRC = PKG / "csrc"
 INCLUDE = PKG.parent / "include"
 LIB = PKG / "libspecattn.so"
 OBJ = PKG / "_build"
-SOURCES = ["api.cu", "select_topp.cu", "sparse_verify.cu"]
+SOURCES = ["api.cu", "select_topp.cu", "sparse_verify.cu", "kv4_rows.cu", "kv4_verify.cu", "evict.cu"]
 FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
          "-Xcompiler", "-fPIC", "-I", str(INCLUDE), "-I", str(CSRC)]
 
