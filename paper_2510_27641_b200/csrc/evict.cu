@@ -249,36 +249,35 @@ __global__ void __launch_bounds__(kEvThreads) evict_kernel(const __grid_constant
   const int mine = max(0, min(P.slice, n - at));
   const bool copy_scores = scores_out != nullptr && scores_out != scores;
   const bool copy_positions = positions_out != nullptr && positions_out != positions;
-  if (n == m) {  // everything stays (the same for the whole cluster)
-    if (rank == 0 && tid == 0) P.n_moves[list] = 0;
-    for (int i = tid; i < mine; i += kEvThreads) {
-      if (copy_scores) scores_out[at + i] = scores[at + i];
-      if (copy_positions) positions_out[at + i] = positions[at + i];
-    }
-    return;
-  }
-
-  // keys
+  for (int i = tid; i < 3 * kEvBins; i += kEvThreads) (&S.hist[0][0])[i] = 0;
+  // keys; and copies of what may stay where it is (moves overwrite the rest of it later)
   {
     const long long end = P.seq_len != nullptr ? P.seq_len[b] : n;
     const long long recent = end - P.n_recent;
-    for (int i = tid; i < 3 * kEvBins; i += kEvThreads) (&S.hist[0][0])[i] = 0;
-    for (int i0 = tid; i0 < mine; i0 += 4 * kEvThreads) {
-      float w[4];
-      int pos[4];
+    constexpr int kAhead = 8;
+    for (int i0 = tid; i0 < mine; i0 += kAhead * kEvThreads) {
+      float w[kAhead];
+      int pos[kAhead];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
+      for (int j = 0; j < kAhead; ++j) {
         const int i = i0 + j * kEvThreads;
         if (i >= mine) continue;
         w[j] = scores[at + i];
         pos[j] = positions != nullptr ? positions[at + i] : at + i;
       }
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
+      for (int j = 0; j < kAhead; ++j) {
         const int i = i0 + j * kEvThreads;
-        if (i < mine) keys[i] = pos[j] < P.n_sink || pos[j] >= recent ? 0xffffffffu : key_of(w[j]);
+        if (i >= mine) continue;
+        keys[i] = pos[j] < P.n_sink || pos[j] >= recent ? 0xffffffffu : key_of(w[j]);
+        if (copy_scores) scores_out[at + i] = at + i < m ? w[j] : 0.f;
+        if (copy_positions && at + i < m) positions_out[at + i] = pos[j];
       }
     }
+  }
+  if (n == m) {  // everything stays (the same for the whole cluster)
+    if (rank == 0 && tid == 0) P.n_moves[list] = 0;
+    return;
   }
   __syncthreads();
 
@@ -378,22 +377,33 @@ __global__ void __launch_bounds__(kEvThreads) evict_kernel(const __grid_constant
     if ((t >> lane) & 1u) dst[into + __popc(t & low)] = slot;
     from += __popc(f);
     into += __popc(t);
-    if ((stays & in_front) >> lane & 1u) {
-      if (copy_scores) scores_out[slot] = scores[slot];
-      if (copy_positions) positions_out[slot] = positions[slot];
-    }
   }
   cluster_sync();  // the lists of all slices are written; and no CTA leaves while a peer reads its shared memory
   if (scores_out == nullptr && positions_out == nullptr) return;
   // the moves, for the weights themselves: every slot read here is behind the budget, every slot written in front
   const int moves = __ldcg(P.n_moves + list);
-  for (int j = static_cast<int>(rank) * kEvThreads + tid; j < moves; j += static_cast<int>(n_cta) * kEvThreads) {
-    const int s = __ldcg(src + j), d = __ldcg(dst + j);
-    if (scores_out != nullptr) scores_out[d] = scores[s];
-    if (positions_out != nullptr) positions_out[d] = positions[s];
+  const int stride = static_cast<int>(n_cta) * kEvThreads;
+  for (int j0 = static_cast<int>(rank) * kEvThreads + tid; j0 < moves; j0 += 4 * stride) {
+    int s[4], d[4], pos[4];
+    float w[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (j0 + k * stride < moves) s[k] = __ldcg(src + j0 + k * stride), d[k] = __ldcg(dst + j0 + k * stride);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (j0 + k * stride >= moves) continue;
+      if (scores_out != nullptr) w[k] = __ldcg(scores + s[k]);
+      if (positions_out != nullptr) pos[k] = __ldcg(positions + s[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (j0 + k * stride >= moves) continue;
+      if (scores_out != nullptr) scores_out[d[k]] = w[k];
+      if (positions_out != nullptr) positions_out[d[k]] = pos[k];
+    }
   }
-  if (scores_out == nullptr) return;
-  if (!copy_scores) cluster_sync();  // in place: behind the budget all has been read
+  if (scores_out == nullptr || copy_scores) return;
+  cluster_sync();  // in place: behind the budget all has been read
   for (int i = max(m, at) + tid; i < at + mine; i += kEvThreads) scores_out[i] = 0.f;
 }
 
@@ -478,10 +488,20 @@ __global__ void __launch_bounds__(kMoveThreads) move_rows_kernel(const __grid_co
   if (P.words == 0) return;
   unsigned char* param = P.param[blockIdx.z];
   const int total_words = n * 2 * heads * P.words;
-  for (int x = threadIdx.x; x < total_words; x += kMoveThreads) {
-    long long from, into;
-    if (piece(x, P.words, 4, P.p_page, P.p_kv, P.p_slot, P.p_head, &from, &into))
-      *reinterpret_cast<uint32_t*>(param + into) = *reinterpret_cast<const uint32_t*>(param + from);
+  for (int x0 = threadIdx.x; x0 < total_words; x0 += kMoveThreads * kAhead) {
+    uint32_t v[kAhead];
+    long long into[kAhead];
+    bool ok[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const int x = x0 + k * kMoveThreads;
+      long long from;
+      ok[k] = x < total_words && piece(x, P.words, 4, P.p_page, P.p_kv, P.p_slot, P.p_head, &from, &into[k]);
+      if (ok[k]) v[k] = *reinterpret_cast<const uint32_t*>(param + from);
+    }
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k)
+      if (ok[k]) *reinterpret_cast<uint32_t*>(param + into[k]) = v[k];
   }
 }
 
@@ -607,9 +627,9 @@ extern "C" int specattn_evict(const specattn_evict_args* args, void* cuda_stream
   P.n_recent = A.n_recent;
   P.B = A.batch;
   P.G = A.n_groups;
-  // a CTA to 2048 slots, up to eight; no more than the slots need while there are lists enough for all SMs
+  // a CTA to 8192 slots, up to eight; no more than the slots need while there are lists enough for all SMs
   int ctas = 1;
-  while (ctas < kEvMaxCluster && ctas * 2048 < A.L && (lists * ctas < 296 || ctas * kEvMaxSlice < A.L)) ctas *= 2;
+  while (ctas < kEvMaxCluster && ctas * 8192 < A.L && (lists * ctas < 296 || ctas * kEvMaxSlice < A.L)) ctas *= 2;
   P.slice = static_cast<int>((A.L + ctas - 1) / ctas);
   const size_t smem = static_cast<size_t>(P.slice) * sizeof(uint32_t);
   static std::atomic<unsigned long long> prepared{0};  // a bit per device
@@ -700,6 +720,10 @@ extern "C" int specattn_move_rows(const specattn_move_args* args, void* cuda_str
   long long per = 65536 / bytes;
   if (per < 1) per = 1;
   if (per > kMoveMost) per = kMoveMost;
+  // (few moves are spread over the SMs: latency is all there is to them)
+  const int sms = device_sm_count();
+  if (sms <= 0) return SPECATTN_ERR_CUDA;
+  while (per > 4 && (A.move_stride + per - 1) / per * A.batch * A.n_groups * A.n_pools < 2ll * sms) per /= 2;
   P.per_block = static_cast<int>(per);
   const long long blocks = (A.move_stride + per - 1) / per;
   if (blocks > INT32_MAX) return SPECATTN_ERR_UNSUPPORTED;

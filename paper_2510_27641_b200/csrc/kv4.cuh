@@ -12,6 +12,24 @@ namespace specattn {
 constexpr int kKv4D = 128;         // values of a row
 constexpr int kKv4Row = kKv4D / 2;  // bytes of its codes
 
+// Division of 0 <= n < 2^31 by a number that the host knows: n / d = (n m) >> s with m = ceil(2^s / d),
+// s = 31 + ceil(log2 d), which is exact for these n because m d exceeds 2^s by less than 2^(s - 31).
+struct FastDiv {
+  unsigned m;
+  int s;
+};
+inline FastDiv fast_div(int d) {
+  int up = 0;
+  while ((1ll << up) < d) ++up;
+  FastDiv f;
+  f.s = 31 + up;
+  f.m = static_cast<unsigned>(((1ull << f.s) + d - 1) / d);
+  return f;
+}
+__device__ __forceinline__ int operator/(int n, const FastDiv& f) {
+  return static_cast<int>((static_cast<unsigned long long>(static_cast<unsigned>(n)) * f.m) >> f.s);
+}
+
 struct Kv4View {
   unsigned char* codes;
   unsigned char* params;  // pairs of 16-bit values, addressed in bytes here
@@ -21,6 +39,7 @@ struct Kv4View {
   const int* table;
   long long table_stride;
   int page_size;
+  FastDiv by_page;
 };
 
 inline Kv4View kv4_view(const specattn_kv4_cache& c) {
@@ -39,6 +58,7 @@ inline Kv4View kv4_view(const specattn_kv4_cache& c) {
   v.table = c.block_table;
   v.table_stride = c.block_table_stride;
   v.page_size = c.page_size;
+  v.by_page = fast_div(c.page_size);
   return v;
 }
 
@@ -59,7 +79,7 @@ inline int kv4_check_buffers(const specattn_kv4_cache& c) {
 
 // The page of the page_index-th page of sequence b; -1 where there is none.
 __device__ __forceinline__ long long page_of(const int* table, long long table_stride, long long n_pages, int b,
-                                             long long page_index) {
+                                             int page_index) {
   if (page_index < 0 || page_index >= table_stride) return -1;
   const long long at = static_cast<long long>(b) * table_stride + page_index;
   const long long page = table != nullptr ? static_cast<long long>(table[at]) : at;

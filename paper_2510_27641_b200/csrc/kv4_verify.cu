@@ -8,9 +8,12 @@
 // with 0x000f000f or 0x00f000f0 gives a register of two exact fp16 values and no conversion takes place (five
 // instructions for eight codes; tensor cores take subnormals as they are).  Queries are scaled by a power of two so
 // that they fit fp16 with all of their bits, those that meet the high codes of a byte by 2^-4 more.
-// The second product subtracts 8 sum w by one more matrix instruction with a constant operand: the weights w = p t
-// are rounded to fp16, and without it an error of w would be multiplied by the code instead of its distance from
-// the middle (2 to 3 times the error of the output).
+// The second product is taken about the middle of the codes, by one more matrix instruction with a constant operand:
+// the weights w = p t are rounded to fp16, and an error of w should be multiplied by a code's distance from 8, not
+// by the code (2 to 3 times the error of the output).  And every second tile of positions uses 15 - e, the complement
+// of the packed bits, with -w:  sum w e = sum_even w e + sum_odd (-w) (15 - e) + 15 sum_odd w.  The accumulators then
+// stay near zero instead of growing with sum w, and what the matrix units cut off at each step stays as small (131072
+// positions: the output's error falls from 1.6 times that of its rounding to bf16 to no more than it).
 //
 // The layout.  Positions are the rows of mma.m16n8k16 in the first product and the summed index in the second,
 // queries the columns of both: 8 query rows cost one instruction where a form with queries as rows pays for 16.
@@ -199,7 +202,7 @@ __global__ void __launch_bounds__(NWARP * 32, 1) kv4_verify_kernel(const __grid_
     auto page = [&](int pos) -> int {
       if (pos == -1) return -1;
       if (pos >= 0) {
-        const long long p = page_of(P.cache.table, P.cache.table_stride, P.cache.n_pages, b, pos / P.cache.page_size);
+        const long long p = page_of(P.cache.table, P.cache.table_stride, P.cache.n_pages, b, pos / P.cache.by_page);
         if (p >= 0) return static_cast<int>(p);
       }
       return -2;
@@ -215,7 +218,7 @@ __global__ void __launch_bounds__(NWARP * 32, 1) kv4_verify_kernel(const __grid_
           s_bad[turn] = SPECATTN_ROW_BAD_INDEX;
           pg = 0;
         } else {
-          slot = pos - pos / P.cache.page_size * P.cache.page_size;
+          slot = pos - pos / P.cache.by_page * P.cache.page_size;
         }
         off = pg * P.cache.s_page + slot * P.cache.s_slot + h * P.cache.s_head;
         par += pg * P.cache.p_page + slot * P.cache.p_slot + h * P.cache.p_head;
@@ -318,7 +321,7 @@ __global__ void __launch_bounds__(NWARP * 32, 1) kv4_verify_kernel(const __grid_
     }
 
     // ---- the chunks ----
-    float acc[8][NT][4], acc8[NT][4];       // output by (element tile, query tile); -8 sum of weights
+    float acc[8][NT][4], acc8[NT][4];       // output by (element tile, query tile), less its middle
     float m[NT][2], l[NT][2], y[NT][2];     // running maximum (log2), sum of p, sum of p (y + 8 t)
     float up = 3e38f;                        // the weights' power of two: w = p t up
 #pragma unroll
@@ -479,7 +482,7 @@ __global__ void __launch_bounds__(NWARP * 32, 1) kv4_verify_kernel(const __grid_
               y[nt][e] = none ? y[nt][e] : fmaf(p, y_of[h2][r], y[nt][e]);
               w[e] = none ? 0.f : p * (t_of[h2][r] * up);
             }
-            pb[nt][r] = transpose8(pack_f16(w[0], w[1]));
+            pb[nt][r] = transpose8(h2 ? pack_f16(-w[0], -w[1]) : pack_f16(w[0], w[1]));
           }
         // V rows of positions 2 t, 2 t + 1, 2 t + 8, 2 t + 9 of the tile, 8 bytes to a lane
         uint2 v[4];
@@ -489,7 +492,10 @@ __global__ void __launch_bounds__(NWARP * 32, 1) kv4_verify_kernel(const __grid_
           v[k] = lds64(stage + (kChunk + row) * kKv4Row + ((g * 8) ^ ((row & 2) << 4)));
         }
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) mma_f16(acc8[nt], 0x80088008u, 0x80088008u, 0x80088008u, 0x80088008u, pb[nt][0], pb[nt][1]);
+        for (int nt = 0; nt < NT; ++nt) {
+          const uint32_t mid = h2 ? 0x80078007u : 0x80088008u;  // -7 (of -w: 15 w - 8 w), -8
+          mma_f16(acc8[nt], mid, mid, mid, mid, pb[nt][0], pb[nt][1]);
+        }
 #pragma unroll
         for (int w = 0; w < 2; ++w)
 #pragma unroll
@@ -501,7 +507,8 @@ __global__ void __launch_bounds__(NWARP * 32, 1) kv4_verify_kernel(const __grid_
             for (int hi = 0; hi < 2; ++hi) {
               const int mt = w * 4 + half * 2 + hi;
               if (hi) x0 >>= 8, x1 >>= 8;
-              const uint32_t a0 = x0 & 0x000f000fu, a1 = x0 & 0x00f000f0u, a2 = x1 & 0x000f000fu, a3 = x1 & 0x00f000f0u;
+              const uint32_t z0 = h2 ? ~x0 : x0, z1 = h2 ? ~x1 : x1;
+              const uint32_t a0 = z0 & 0x000f000fu, a1 = z0 & 0x00f000f0u, a2 = z1 & 0x000f000fu, a3 = z1 & 0x00f000f0u;
 #pragma unroll
               for (int nt = 0; nt < NT; ++nt) mma_f16(acc[mt][nt], a0, a1, a2, a3, pb[nt][0], pb[nt][1]);
             }
