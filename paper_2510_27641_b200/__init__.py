@@ -94,7 +94,7 @@ class Kv4VerifyArgs(C.Structure):
                 ("counts", C.c_void_p), ("sm_scale", C.c_float), ("out_f32", C.c_int32),
                 ("out", C.c_void_p), ("lse", C.c_void_p), ("status", C.c_void_p),
                 ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t), ("tail_len", C.c_int32),
-                ("reserved", C.c_int32)]
+                ("flags", C.c_uint32)]
 
 
 class AccumulateArgs(C.Structure):

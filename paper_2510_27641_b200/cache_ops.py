@@ -166,14 +166,14 @@ def kv4_verify(q: torch.Tensor, codes: torch.Tensor, params: torch.Tensor, kv_le
                block_table: torch.Tensor | None = None, pages_per_seq: int | None = None, idx: torch.Tensor | None = None,
                counts: torch.Tensor | None = None, n_groups: int = 1, dense: bool = False, sm_scale: float = 0.0,
                tail_len: int = 0, out: torch.Tensor | None = None, lse: torch.Tensor | None = None,
-               status: torch.Tensor | None = None, workspace: torch.Tensor | None = None, stream=None):
+               status: torch.Tensor | None = None, workspace: torch.Tensor | None = None, flags: int = 0, stream=None):
     """specattn_kv4_verify for one target layer: attention of q [B, T, H_q, 128] (of the type of ``params``) over the listed
     positions (idx [B, n_groups, stride], counts [B, n_groups]; all positions where ``dense``) and the tail of a 4-bit
     cache.  Returns (out [B, T, H_q, 128] of q's type, or float32 where ``out`` is, lse f32 [B, T, H_q], status)."""
     index = _device(q, codes, params, kv_len, block_table, None if dense else idx, None if dense else counts, out, lse, status, workspace)
     shape = q.shape
     # (out, lse and the workspace are made here or looked at by every call)
-    key = (shape, q.dtype, n_groups, dense, sm_scale, tail_len, out is not None and out.dtype is _F32, index,
+    key = (shape, q.dtype, n_groups, dense, sm_scale, tail_len, flags, out is not None and out.dtype is _F32, index,
            None if dense else idx.shape) + _cache_key(codes, params, block_table, pages_per_seq)
 
     def make():
@@ -187,7 +187,7 @@ def kv4_verify(q: torch.Tensor, codes: torch.Tensor, params: torch.Tensor, kv_le
         if not dense:
             assert idx.dim() == 3 and idx.shape[0] == b and idx.shape[1] == n_groups, "idx: [B, n_groups, stride] expected"
             a.idx_stride = idx.shape[2]
-        a.sm_scale, a.tail_len = float(sm_scale), int(tail_len)
+        a.sm_scale, a.tail_len, a.flags = float(sm_scale), int(tail_len), int(flags)
         return a, a.cache, C.byref(a), kv4_verify_workspace_bytes(q, codes) if b > 0 else 256, (b, t, hq)
 
     a, c, ref, need, rows = _calls.get(key, make)

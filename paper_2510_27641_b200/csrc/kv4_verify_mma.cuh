@@ -1,0 +1,370 @@
+// The path of specattn_kv4_verify on mma.sync.
+//
+// The layout.  Positions are the rows of mma.m16n8k16 in the first product and the summed index in the second,
+// queries the columns of both: 8 query rows cost one instruction where a form with queries as rows pays for 16.
+// Which element of a row, and which of a tile's positions, goes to which lane is free as long as both operands
+// agree, so a lane reads 16 bytes of a K row and 8 bytes of a V row as they lie in the cache.  Probabilities change
+// from result to operand layout by movmatrix.
+//
+// The middle of the codes is taken off by one more matrix instruction with a constant operand.  And every second tile of
+// positions uses 15 - e, the complement of the packed bits, with -w:
+//     sum w e = sum_even w e + sum_odd (-w) (15 - e) + 15 sum_odd w.
+// The accumulators then stay near zero instead of growing with sum w, and what the matrix units cut off at each step
+// stays as small (131072 positions: the output's error falls from 1.6 times that of its rounding to bf16 to no more
+// than it).
+//
+// A warp owns chunks of 32 positions from the gather to the running maximum, sum and output, with a ring of its own
+// that cp.async fills: no barrier in the loop.  Warps meet at the end of a unit (sequence, KV head).
+#pragma once
+#include "kv4_verify.cuh"
+
+namespace specattn {
+namespace {
+
+__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+
+template <int NT, int NWARP, int STAGES>
+struct MmaPath {
+  static constexpr int kQueries = NT * 8;
+  static constexpr int kQBytes = NT * 8 * 32 * 8;  // query operand: [tile][step][lane] of two registers
+  static constexpr int kRing = STAGES * kStageBytes;
+  static constexpr int kMeet = NWARP * kQueries * kRowFloats * 4;  // what the warps leave for one another, in the rings' place
+  static constexpr int kSmem = kQBytes + (NWARP * kRing > kMeet ? NWARP * kRing : kMeet);
+};
+
+template <int kQueries>
+struct MmaShared {
+  int bad[2];  // of this segment, and cleared for the next
+  int qmax;
+  float qsum[kQueries];  // times the scale
+  int limit[kQueries];   // how many tail positions a query row sees
+};
+
+template <int NT, int NWARP, int STAGES>
+__device__ __forceinline__ void mma_path(const Kv4Params& P, const Partition& part, unsigned char* smem, MmaShared<NT * 8>& S) {
+  using K = MmaPath<NT, NWARP, STAGES>;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int g = lane >> 2, t = lane & 3;
+  const uint32_t ring_at = smem_u32(smem + K::kQBytes + warp * K::kRing);
+  const Units units = units_of(P, 0);
+  int u = part.unit, u_start = part.start, turn = 0;
+
+  // ---- one segment of a unit after the other ----
+  for (int at = part.first; at < part.last;) {
+    const int rg = u / (P.B * P.H), bh = u - rg * P.B * P.H, b = bh / P.H, h = bh - b * P.H;
+    const Gather G(P, b, h);
+    const int n_list = G.n_list, n_chunks = (G.n_all + kChunk - 1) / kChunk;
+    const int seg0 = at - u_start, seg1 = min(n_chunks, part.last - u_start);  // chunks of the unit
+    const int row0 = rg * units.rows, n_rows = min(units.rows, P.rows - row0);
+
+    auto position = [&](int chunk) { return chunk < seg1 ? G.position(chunk * kChunk + lane) : -1; };
+    auto fetch = [&](int chunk, int pos, int pg) {
+      // K rows lie in order.  Row j of a V tile of 16 lies where the second product's lanes find it without bank
+      // conflicts: 2 t -> t, 2 t + 1 -> t + 4 within eight, its 32-byte halves swapped by bit 1.
+      G.fetch(ring_at + ((chunk / NWARP) % STAGES) * kStageBytes, pos, pg, lane, &S.bad[turn],
+              [](int row, int piece) { return row * kKv4Row + piece * 16; },
+              [](int row, int piece) {
+                const int r8 = row & 7, at_row = (row & ~7) | ((r8 >> 1) | ((r8 & 1) << 2));
+                return at_row * kKv4Row + ((piece * 16) ^ ((at_row & 2) << 4));
+              });
+    };
+
+    // the first chunks are on their way before the queries are read
+    const int first = seg0 + ((warp - seg0) % NWARP + NWARP) % NWARP;  // this warp's: chunk % NWARP == warp
+    int pos_next, pg_next, pos_then;  // of chunk + (STAGES - 1) NWARP; of the one behind it
+    {
+      int pos[STAGES + 1], pg[STAGES];
+#pragma unroll
+      for (int s = 0; s <= STAGES; ++s) pos[s] = position(first + s * NWARP);
+#pragma unroll
+      for (int s = 0; s < STAGES; ++s) pg[s] = G.page(pos[s]);
+#pragma unroll
+      for (int s = 0; s < STAGES - 1; ++s) {
+        if (first + s * NWARP < seg1) fetch(first + s * NWARP, pos[s], pg[s]);
+        cp_commit();
+      }
+      pos_next = pos[STAGES - 1];
+      pg_next = pg[STAGES - 1];
+      pos_then = pos[STAGES];
+    }
+
+    // ---- queries ----
+    if (tid == 0) S.qmax = 0;
+    __syncthreads();
+    if (tid == 0) S.bad[turn ^ 1] = 0;
+    look_at_queries<NWARP, K::kQueries>(P, b, h, row0, n_rows, &S.qmax, S.qsum, S.limit);
+    __syncthreads();
+    const int qexp = query_exponent(S.qmax);
+    const float q_up = __int_as_float((127 + qexp) << 23);
+    // step 2 w meets codes 0, 4 (low halves of bytes) and 1, 5 (high) of word w of the lane's 16 bytes, step 2 w + 1
+    // codes 2, 6 and 3, 7
+    for (int i = tid; i < NT * 4 * 32; i += NWARP * 32) {
+      const int nt = i >> 7, w = (i >> 5) & 3, l = i & 31, r = nt * 8 + (l >> 2);
+      uint4 x = make_uint4(0u, 0u, 0u, 0u);
+      if (r < n_rows) x = query_word(P, query_at(P, b, h, row0 + r) + (l & 3) * 32 + w * 8, q_up);
+      uint2* to = reinterpret_cast<uint2*>(smem) + (nt * 8 + 2 * w) * 32 + l;
+      to[0] = make_uint2(x.x, x.y);
+      to[32] = make_uint2(x.z, x.w);
+    }
+    __syncthreads();
+    const float k_mul = P.scale * 16777216.f * __int_as_float((127 - qexp) << 23);  // codes are c 2^-24 in the product
+    float sq[NT][2], m[NT][2], l[NT][2], y[NT][2];  // sum q; running maximum (log2), sum of p, sum of p (y + 8 t)
+    float acc[8][NT][4], acc8[NT][4];                // output by (element tile, query tile), less its middle
+    float up = 3e38f;                                // the weights' power of two: w = p t up
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        acc8[nt][e] = 0.f;
+#pragma unroll
+        for (int mt = 0; mt < 8; ++mt) acc[mt][nt][e] = 0.f;
+      }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) sq[nt][e] = S.qsum[nt * 8 + 2 * t + e], m[nt][e] = 0.f, l[nt][e] = 0.f, y[nt][e] = 0.f;
+    }
+    const uint2* q_op = reinterpret_cast<const uint2*>(smem) + lane;
+
+#pragma unroll 1
+    for (int chunk = first; chunk < seg1; chunk += NWARP) {
+      cp_wait<STAGES - 2>();
+      __syncwarp();
+      {
+        const int ahead = chunk + (STAGES - 1) * NWARP;
+        if (ahead < seg1) fetch(ahead, pos_next, pg_next);
+        cp_commit();
+        pos_next = pos_then;
+        pg_next = G.page(pos_then);
+        pos_then = position(ahead + 2 * NWARP);
+      }
+      const uint32_t stage = ring_at + ((chunk / NWARP) % STAGES) * kStageBytes;
+
+      // first product: scores of two tiles of 16 positions
+      float s[2][NT][4];
+#pragma unroll
+      for (int h2 = 0; h2 < 2; ++h2)
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[h2][nt][e] = 0.f;
+      {
+        uint32_t ka[2][2][4];
+#pragma unroll
+        for (int h2 = 0; h2 < 2; ++h2)
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            const uint4 x = lds128(stage + (h2 * 16 + r * 8 + g) * kKv4Row + t * 16);
+            ka[h2][r][0] = x.x, ka[h2][r][1] = x.y, ka[h2][r][2] = x.z, ka[h2][r][3] = x.w;
+          }
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+#pragma unroll
+          for (int hi = 0; hi < 2; ++hi) {
+            uint32_t a[2][4];
+#pragma unroll
+            for (int h2 = 0; h2 < 2; ++h2) {
+              const uint32_t x0 = hi ? ka[h2][0][w] >> 8 : ka[h2][0][w], x1 = hi ? ka[h2][1][w] >> 8 : ka[h2][1][w];
+              a[h2][0] = x0 & 0x000f000fu, a[h2][1] = x1 & 0x000f000fu;
+              a[h2][2] = x0 & 0x00f000f0u, a[h2][3] = x1 & 0x00f000f0u;
+            }
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+              const uint2 qb = q_op[(nt * 8 + 2 * w + hi) * 32];
+#pragma unroll
+              for (int h2 = 0; h2 < 2; ++h2) mma_f16(s[h2][nt], a[h2][0], a[h2][1], a[h2][2], a[h2][3], qb.x, qb.y);
+            }
+          }
+      }
+
+      // scales: (s, z) and (t, y) of the positions g and g + 8 of both tiles; scores from the running maximum on
+      float t_of[2][2], y_of[2][2], t_max = 0.f;
+#pragma unroll
+      for (int h2 = 0; h2 < 2; ++h2)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          const uint2 x = lds64(stage + 2 * kChunk * kKv4Row + (h2 * 16 + r * 8 + g) * 8);
+          const float2 kp = widen16(x.x, P.half), vp = widen16(x.y, P.half);
+          const float ks = kp.x * k_mul;
+          t_of[h2][r] = vp.x;
+          y_of[h2][r] = fmaf(8.f, vp.x, vp.y);
+          t_max = fmaxf(t_max, fabsf(vp.x));
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) s[h2][nt][2 * r + e] = fmaf(s[h2][nt][2 * r + e], ks, fmaf(kp.y, sq[nt][e], -m[nt][e]));
+        }
+      // what a query does not see: past the end, or behind it in the tail.  (A masked row may hold anything, and 0 NaN is
+      // NaN: what a tail row's V scale would spoil, its scores spoil instead.)
+      const int i0 = chunk * kChunk;
+      if (i0 + kChunk > n_list) {
+#pragma unroll
+        for (int h2 = 0; h2 < 2; ++h2)
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            const int i = i0 + h2 * 16 + r * 8 + g;
+            const bool spoilt = i >= n_list && !(fabsf(t_of[h2][r]) <= FLT_MAX && fabsf(y_of[h2][r]) <= FLT_MAX);
+            if (spoilt) t_of[h2][r] = y_of[h2][r] = 0.f;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                if (spoilt) s[h2][nt][2 * r + e] = NAN;
+                if (i >= n_list + S.limit[nt * 8 + 2 * t + e]) s[h2][nt][2 * r + e] = -INFINITY;
+              }
+          }
+      }
+      // the maximum moves only where a score passes it by 2^8, the weights' scale where one passes 64
+      float top = s[0][0][0];
+#pragma unroll
+      for (int h2 = 0; h2 < 2; ++h2)
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) top = fmaxf(top, s[h2][nt][e]);
+      if (__any_sync(0xffffffffu, top > 8.f || t_max * up > 64.f || chunk == first)) {
+        t_max = t_max <= FLT_MAX ? t_max : 0.f;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) t_max = fmaxf(t_max, __shfl_xor_sync(0xffffffffu, t_max, o));
+        // t_max up in [32, 64)
+        float up_now = up;
+        if (t_max > 0.f) up_now = fminf(up, __int_as_float((127 + min(5 + 127 - (__float_as_int(t_max) >> 23), 100)) << 23));
+        const float scale_now = up_now / up;
+        up = up_now;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          float f[2];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            float v = fmaxf(fmaxf(s[0][nt][e], s[0][nt][2 + e]), fmaxf(s[1][nt][e], s[1][nt][2 + e]));
+            v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 4));
+            v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 8));
+            v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 16));
+            // (a query that sees nothing of the warp's first chunk sees nothing of the later ones)
+            const float d = chunk == first ? (v == -INFINITY ? 0.f : v) : fmaxf(v, 0.f);
+            f[e] = ex2(-d);
+            m[nt][e] += d;
+            l[nt][e] *= f[e];
+            y[nt][e] *= f[e];
+            f[e] = chunk == first ? 0.f : f[e] * scale_now;
+            s[0][nt][e] -= d, s[0][nt][2 + e] -= d, s[1][nt][e] -= d, s[1][nt][2 + e] -= d;
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            acc8[nt][e] *= f[e & 1];
+#pragma unroll
+            for (int mt = 0; mt < 8; ++mt) acc[mt][nt][e] *= f[e & 1];
+          }
+        }
+      }
+
+      // weights, and the second product
+#pragma unroll
+      for (int h2 = 0; h2 < 2; ++h2) {
+        uint32_t pb[NT][2];
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          const float w_of = h2 ? -t_of[h2][r] * up : t_of[h2][r] * up;
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            const float p0 = ex2(s[h2][nt][2 * r]), p1 = ex2(s[h2][nt][2 * r + 1]);
+            l[nt][0] += p0, l[nt][1] += p1;
+            y[nt][0] = fmaf(p0, y_of[h2][r], y[nt][0]), y[nt][1] = fmaf(p1, y_of[h2][r], y[nt][1]);
+            pb[nt][r] = transpose8(pack_f16(p0 * w_of, p1 * w_of));
+          }
+        }
+        // V rows of positions 2 t, 2 t + 1, 2 t + 8, 2 t + 9 of the tile, 8 bytes to a lane
+        uint2 v[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int row = h2 * 16 + (k >> 1) * 8 + (k & 1) * 4 + t;
+          v[k] = lds64(stage + (kChunk + row) * kKv4Row + ((g * 8) ^ ((row & 2) << 4)));
+        }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          const uint32_t mid = h2 ? 0x80078007u : 0x80088008u;  // -7 (of -w: 15 w - 8 w), -8
+          mma_f16(acc8[nt], mid, mid, mid, mid, pb[nt][0], pb[nt][1]);
+        }
+#pragma unroll
+        for (int w = 0; w < 2; ++w)
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            const uint32_t sel = half ? 0x7632u : 0x5410u;
+            uint32_t x0 = w ? __byte_perm(v[0].y, v[1].y, sel) : __byte_perm(v[0].x, v[1].x, sel);
+            uint32_t x1 = w ? __byte_perm(v[2].y, v[3].y, sel) : __byte_perm(v[2].x, v[3].x, sel);
+#pragma unroll
+            for (int hi = 0; hi < 2; ++hi) {
+              const int mt = w * 4 + half * 2 + hi;
+              if (hi) x0 >>= 8, x1 >>= 8;
+              const uint32_t z0 = h2 ? ~x0 : x0, z1 = h2 ? ~x1 : x1;
+              const uint32_t a0 = z0 & 0x000f000fu, a1 = z0 & 0x00f000f0u, a2 = z1 & 0x000f000fu, a3 = z1 & 0x00f000f0u;
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) mma_f16(acc[mt][nt], a0, a1, a2, a3, pb[nt][0], pb[nt][1]);
+            }
+          }
+      }
+    }
+    cp_wait<0>();
+    __syncthreads();  // the rings are free
+
+    // ---- the warps' parts meet ----
+    float* meet = reinterpret_cast<float*>(smem + K::kQBytes);
+    {
+      const float down = 1.f / up;  // (0 where the warp has seen nothing: its sums are 0)
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          float ls = l[nt][e], ys = y[nt][e];
+#pragma unroll
+          for (int o = 4; o < 32; o <<= 1) {
+            ls += __shfl_xor_sync(0xffffffffu, ls, o);
+            ys += __shfl_xor_sync(0xffffffffu, ys, o);
+          }
+          float* rec = meet + (warp * K::kQueries + nt * 8 + 2 * t + e) * kRowFloats;
+          if (g == 0) rec[kKv4D] = ls == 0.f ? -FLT_MAX : m[nt][e], rec[kKv4D + 1] = ls;
+          const float mid = acc8[nt][e];
+          // lane g has elements 16 g ... 16 g + 15: tile mt holds 2 mt (codes in the low half of a byte) and 2 mt + 1
+#pragma unroll
+          for (int mt = 0; mt < 8; mt += 2) {
+            float4 o4;
+            o4.x = fmaf((acc[mt][nt][e] + mid) * 16777216.f, down, ys);
+            o4.y = fmaf(fmaf(acc[mt][nt][2 + e], 1048576.f, mid * 16777216.f), down, ys);
+            o4.z = fmaf((acc[mt + 1][nt][e] + mid) * 16777216.f, down, ys);
+            o4.w = fmaf(fmaf(acc[mt + 1][nt][2 + e], 1048576.f, mid * 16777216.f), down, ys);
+            *reinterpret_cast<float4*>(rec + 16 * g + 2 * mt) = o4;
+          }
+        }
+    }
+    __syncthreads();
+    const bool whole = seg0 == 0 && seg1 == n_chunks;
+    float* rec = P.partial + static_cast<long long>(2 * blockIdx.x + (seg0 == 0 ? 1 : 0)) * units.rows * kRowFloats;
+    finish<NWARP, NWARP, K::kQueries>(P, meet, b, h, row0, n_rows, whole, rec);
+    if (tid == 0) {
+      if (whole)
+        P.flags[u] = S.bad[turn];
+      else
+        rec[kKv4D + 2] = __int_as_float(S.bad[turn]);
+    }
+    turn ^= 1;
+    __syncthreads();  // the records have been read
+    at = u_start + seg1;
+    if (seg1 == n_chunks) {
+      u_start += n_chunks;
+      do {
+        ++u;
+      } while (u < units.n && at < part.last && chunks_of(P, u, kChunk) == 0);
+    }
+  }
+}
+
+}  // namespace
+}  // namespace specattn

@@ -163,7 +163,16 @@ def _case(seed, B, T, Hq, Hkv, lens, counts, *, page=16, dtype=torch.bfloat16, l
                 tail=tail, dense=dense, lists=per_head)
 
 
-def _run(c, **kw):
+ENGINES = {"auto": 0, "mma.sync": 2, "tcgen05": 4}
+
+
+def _engines(T, Hq, Hkv):
+    """What may run that many query rows."""
+    return ["mma.sync", "tcgen05"] if T * (Hq // Hkv) > 16 else ["auto"]
+
+
+def _run(c, engine="auto", **kw):
+    kw.setdefault("flags", ENGINES[engine])
     up = lambda t: None if t is None else t.to(DEV)
     return _sa().kv4_verify(c["q"].to(DEV), _to_gpu(c["codes"]), _to_gpu(c["params"]), torch.tensor(c["lens"], dtype=torch.int32, device=DEV),
                             block_table=up(c["table"]), pages_per_seq=c["pps"], idx=up(c["idx"]), counts=up(c["counts"]),
@@ -189,9 +198,10 @@ HEADS = [(1, 8, 8), (1, 32, 8), (6, 32, 8), (5, 64, 8), (8, 8, 1), (1, 64, 1), (
 @pytest.mark.parametrize("lens,counts", LENGTHS)
 def test_attention_over_lists(lens, counts, T, Hq, Hkv):
     c = _case(11 + T, len(lens), T, Hq, Hkv, lens, counts, dtype=torch.float16 if T % 2 else torch.bfloat16)
-    out, lse, _ = _run(c)
-    assert out.dtype is c["q"].dtype
-    _check(c, out, lse)
+    for engine in _engines(T, Hq, Hkv):
+        out, lse, _ = _run(c, engine)
+        assert out.dtype is c["q"].dtype
+        _check(c, out, lse)
 
 
 @pytest.mark.parametrize("T,Hq,Hkv,lens,tail,page,layout", [
@@ -205,15 +215,17 @@ def test_attention_over_lists(lens, counts, T, Hq, Hkv):
 @pytest.mark.parametrize("paged", [True, False])
 def test_attention_over_everything_with_a_tail(T, Hq, Hkv, lens, tail, page, layout, paged):
     c = _case(23, len(lens), T, Hq, Hkv, lens, None, dense=True, tail=tail, page=page, layout=layout, paged=paged)
-    out, lse, _ = _run(c)
-    _check(c, out, lse)
+    for engine in _engines(T, Hq, Hkv):
+        out, lse, _ = _run(c, engine)
+        _check(c, out, lse)
 
 
 @pytest.mark.parametrize("T,Hq,Hkv", [(1, 16, 4), (6, 32, 8), (5, 64, 8)])
 def test_a_list_per_kv_head(T, Hq, Hkv):
     c = _case(31, 3, T, Hq, Hkv, [400, 60, 900], [300, 5, 611], G=Hkv, tail=T)
-    out, lse, _ = _run(c)
-    _check(c, out, lse)
+    for engine in _engines(T, Hq, Hkv):
+        out, lse, _ = _run(c, engine)
+        _check(c, out, lse)
 
 
 @pytest.mark.parametrize("B,T,Hq,Hkv,count", [(64, 1, 32, 8, 40), (256, 6, 32, 8, 7), (40, 5, 64, 8, 33), (2048, 1, 1, 1, 3), (19, 1, 8, 8, 64)])
@@ -225,7 +237,11 @@ def test_many_units(B, T, Hq, Hkv, count):
         few = list(range(0, B, max(1, B // 12)))
     else:
         few = list(range(B))
-    out, lse, _ = _run(c)
+    for engine in _engines(T, Hq, Hkv):
+        _check_few(c, few, counts, *_run(c, engine)[:2])
+
+
+def _check_few(c, few, counts, out, lse):
     pick = lambda t: t if t is None else t[few]
     sub = dict(c, q=c["q"][few], table=pick(c["table"]), lens=[c["lens"][b] for b in few], lists=[c["lists"][b] for b in few])
     _check(sub, out[few], lse[few])
@@ -233,13 +249,38 @@ def test_many_units(B, T, Hq, Hkv, count):
     assert torch.all(torch.isinf(lse.cpu()[none])) and not out.cpu()[none].any() and torch.all(torch.isfinite(lse.cpu()[~none]))
 
 
-def test_a_long_list_split_over_the_gpu():
-    c = _case(43, 1, 6, 8, 2, [70000], [64007])
+@pytest.mark.parametrize("T,Hq,Hkv,lens,counts", [(6, 8, 2, [70000], [64007]), (5, 32, 4, [9000, 20000], [8999, 12345]), (17, 1, 1, [3000], [2900])])
+def test_long_lists_split_over_the_gpu(T, Hq, Hkv, lens, counts):
+    c = _case(43, len(lens), T, Hq, Hkv, lens, counts)
+    for engine in _engines(T, Hq, Hkv):
+        out, lse, _ = _run(c, engine)
+        _check(c, out, lse)
+
+
+def test_calls_long_enough_for_tcgen05_take_it_by_themselves():
+    c = _case(44, 2, 6, 8, 2, [90000, 80000], None, dense=True)
     out, lse, _ = _run(c)
+    tc, mma = _run(c, "tcgen05"), _run(c, "mma.sync")
+    assert torch.equal(out, tc[0]) and torch.equal(lse, tc[1]) and not torch.equal(lse, mma[1])
+    few = dict(c, q=c["q"][:, :2].contiguous())
+    _check(few, out[:, :2], lse[:, :2])
+
+
+def test_a_bounded_wait_that_runs_out_is_reported():
+    """The first completion of CTA 0 is withheld: its waits run out, the kernel returns, the status says so, and the next call is
+    right."""
+    sa = _sa()
+    c = _case(45, 2, 6, 32, 8, [3000, 2000], None, dense=True)
+    status = torch.zeros(2, dtype=torch.int32, device=DEV)
+    _run(c, status=status, flags=sa.VERIFY_ENGINE_TCGEN05 | sa.VERIFY_TEST_LOSE_ARRIVAL)
+    assert status[0].item() == sa.ROW_TIMEOUT
+    out, lse, _ = _run(c, "tcgen05", status=status)
+    assert status.tolist() == [0, 0]
     _check(c, out, lse)
 
 
-def test_scores_that_grow_and_scales_that_grow():
+@pytest.mark.parametrize("engine", ["mma.sync", "tcgen05"])
+def test_scores_that_grow_and_scales_that_grow(engine):
     """The running maximum and the weights' scale both move along the list: K rows that a query likes more and more,
     V rows whose range spans 2^30."""
     gen, n = _gen(47), 2000
@@ -251,106 +292,112 @@ def test_scores_that_grow_and_scales_that_grow():
         x[page, 0] += (pos / 400.0)[:, None, None] * c["q"][0, 0, 0].float().sign()
         x[page, 1] *= (2.0 ** (30.0 * pos / n - 20))[:, None, None]
     c["codes"], c["params"] = quantise(x.to(torch.bfloat16))
-    out, lse, _ = _run(c)
+    out, lse, _ = _run(c, engine=engine)
     _check(c, out, lse)
     # and the other way round
     for a in ("codes", "params"):
         c[a] = c[a].flip(0).contiguous()
     c["table"] = c["table"].flip(1).contiguous()
-    out, lse, _ = _run(c)
+    out, lse, _ = _run(c, engine=engine)
     _check(c, out, lse)
 
 
-def test_constant_rows_and_rows_far_from_zero():
+@pytest.mark.parametrize("engine", ["mma.sync", "tcgen05"])
+def test_constant_rows_and_rows_far_from_zero(engine):
     c = _case(53, 2, 6, 32, 8, [500, 33], None, dense=True)
     gen = _gen(53)
     x = torch.randn(c["codes"].shape[0], 2, 16, 8, 128, generator=gen)
     x[::3] = x[::3, :, :, :, :1]               # constant rows: scale 0
     x[1::3, 1] = x[1::3, 1] * 2 ** -6 + 40     # far from zero, little range
     c["codes"], c["params"] = quantise(x.to(torch.bfloat16))
-    out, lse, _ = _run(c)
+    out, lse, _ = _run(c, engine=engine)
     _check(c, out, lse)
 
 
 @pytest.mark.parametrize("scale", [2.0 ** -60, 2.0 ** -9, 2.0 ** 40])
-def test_queries_of_any_magnitude(scale):
+@pytest.mark.parametrize("engine", ["mma.sync", "tcgen05"])
+def test_queries_of_any_magnitude(scale, engine):
     """A power of two in the queries and its inverse in sm_scale: bf16's range, beyond fp16's."""
     c = _case(59, 2, 6, 32, 8, [200, 100], [150, 100])
-    out, lse, _ = _run(c)
+    out, lse, _ = _run(c, engine=engine)
     big = dict(c, q=c["q"] * scale)
-    out2, lse2, _ = _run(big, sm_scale=1 / (math.sqrt(128) * scale))
+    out2, lse2, _ = _run(big, engine, sm_scale=1 / (math.sqrt(128) * scale))
     assert torch.equal(out2, out) or float((out2.float() - out.float()).abs().max()) <= 2.0 ** -7
     _check(c, out2, lse2)
 
 
-def test_float32_output_and_given_buffers():
+@pytest.mark.parametrize("engine", ["mma.sync", "tcgen05"])
+def test_float32_output_and_given_buffers(engine):
     sa = _sa()
     c = _case(61, 2, 6, 32, 8, [300, 900], [280, 700])
-    out16, lse16, _ = _run(c)
+    out16, lse16, _ = _run(c, engine=engine)
     out = torch.full(c["q"].shape, float("nan"), device=DEV)
     lse = torch.full(c["q"].shape[:3], float("nan"), device=DEV)
     status = torch.full((2,), 5, dtype=torch.int32, device=DEV)
     ws = torch.full((sa.kv4_verify_workspace_bytes(c["q"].to(DEV), _to_gpu(c["codes"])),), 255, dtype=torch.uint8, device=DEV)
     for _ in range(2):   # the workspace needs no preparation and holds no state
-        _run(c, out=out, lse=lse, status=status, workspace=ws)
+        _run(c, out=out, lse=lse, status=status, workspace=ws, engine=engine)
         assert status.tolist() == [0, 0]
         assert torch.equal(out.to(torch.bfloat16), out16) and torch.equal(lse, lse16)
     _check(c, out, lse)
 
 
-def test_nothing_outside_the_lists_is_looked_at():
+@pytest.mark.parametrize("engine", ["mma.sync", "tcgen05"])
+def test_nothing_outside_the_lists_is_looked_at(engine):
     """Every row that no list names, masked tail rows and ends of pages hold NaN."""
-    c = _case(67, 2, 4, 16, 4, [333, 90], [200, 60], tail=4)
+    c = _case(67, 2, 5, 16, 4, [333, 90], [200, 60], tail=5)
     params = torch.full_like(c["params"], float("nan"))
     for b in range(2):
-        for pos in c["lists"][b][0] + [c["lens"][b] + j for j in range(4)]:
+        for pos in c["lists"][b][0] + [c["lens"][b] + j for j in range(5)]:
             at = int(c["table"][b, pos // 16]), pos % 16
             params[at[0], :, at[1]] = c["params"][at[0], :, at[1]]
     clean = dict(c)
     c["params"] = params
-    out, lse, _ = _run(c)
+    out, lse, _ = _run(c, engine=engine)
     _check(clean, out, lse)
     # the last in-flight row is NaN: only the last query sees it
     for b in range(2):
-        pos = c["lens"][b] + 3
+        pos = c["lens"][b] + 4
         c["params"][int(c["table"][b, pos // 16]), :, pos % 16] = float("nan")
-    out, lse, _ = _run(c)
-    assert torch.all(torch.isfinite(out[:, :3])) and torch.all(torch.isnan(out[:, 3])) and torch.all(torch.isnan(lse[:, 3]))
-    want, want_lse, tol, tol_lse = verify64(clean["q"], clean["codes"], clean["params"], clean["lists"], clean["lens"], 4, 16, clean["table"], clean["pps"])
-    assert torch.all((out.cpu().double() - want)[:, :3].abs() <= tol[:, :3])
+    out, lse, _ = _run(c, engine=engine)
+    assert torch.all(torch.isfinite(out[:, :4])) and torch.all(torch.isnan(out[:, 4])) and torch.all(torch.isnan(lse[:, 4]))
+    want, want_lse, tol, tol_lse = verify64(clean["q"], clean["codes"], clean["params"], clean["lists"], clean["lens"], 5, 16, clean["table"], clean["pps"])
+    assert torch.all((out.cpu().double() - want)[:, :4].abs() <= tol[:, :4])
 
 
-def test_a_query_of_nan_or_infinity_spoils_no_other():
+@pytest.mark.parametrize("engine", ["mma.sync", "tcgen05"])
+def test_a_query_of_nan_or_infinity_spoils_no_other(engine):
     c = _case(71, 1, 6, 32, 8, [200], [150])
-    out, lse, _ = _run(c)
+    out, lse, _ = _run(c, engine=engine)
     for bad in (float("nan"), float("inf")):
         q = c["q"].clone()
         q[0, 2, 5, 17] = bad
-        out2, lse2, _ = _run(dict(c, q=q))
+        out2, lse2, _ = _run(dict(c, q=q), engine=engine)
         keep = torch.ones(6, 32, dtype=torch.bool)
         keep[2, 5] = False
         assert torch.equal(out2[0][keep.to(DEV)], out[0][keep.to(DEV)]) and torch.equal(lse2[0][keep.to(DEV)], lse[0][keep.to(DEV)])
         assert torch.all(torch.isnan(out2[0, 2, 5]))
 
 
-def test_bad_positions_and_pages_are_reported_and_read_from_the_first():
+@pytest.mark.parametrize("engine", ["mma.sync", "tcgen05"])
+def test_bad_positions_and_pages_are_reported_and_read_from_the_first(engine):
     sa = _sa()
-    c = _case(73, 4, 2, 8, 2, [100, 100, 100, 100], [50, 50, 50, 50])
+    c = _case(73, 4, 5, 8, 2, [100, 100, 100, 100], [50, 50, 50, 50])
     c["idx"][1, 0, 7] = 100        # beyond the context
     c["idx"][2, 0, 0] = -5
     c["table"][3, 2] = 10 ** 6     # no such page
     status = torch.zeros(4, dtype=torch.int32, device=DEV)
-    out, lse, _ = _run(c, status=status)
+    out, lse, _ = _run(c, status=status, engine=engine)
     hit = any(32 <= p < 48 for p in c["lists"][3][0])
     assert hit and status.tolist() == [0] + [sa.ROW_BAD_INDEX] * 3
     assert torch.all(torch.isfinite(out))
     first = dict(c, q=c["q"][:1], table=c["table"][:1], lens=[100], lists=c["lists"][:1])
     _check(first, out[:1], lse[:1])
     # a context longer than the block table, dense
-    c = _case(74, 1, 1, 8, 2, [100], None, dense=True)
+    c = _case(74, 1, 5, 8, 2, [100], None, dense=True)
     c["lens"] = [5000]
     status = torch.zeros(1, dtype=torch.int32, device=DEV)
-    out, _, _ = _run(c, status=status)
+    out, _, _ = _run(c, status=status, engine=engine)
     assert status.item() == sa.ROW_BAD_INDEX and torch.all(torch.isfinite(out))
 
 
@@ -382,14 +429,15 @@ def test_rows_beyond_four_gigabytes():
                 table=torch.arange(8).view(2, 4), pps=4), out, lse)
 
 
-def test_the_same_bits_again_on_a_stream_and_in_a_graph():
+@pytest.mark.parametrize("engine", ["mma.sync", "tcgen05"])
+def test_the_same_bits_again_on_a_stream_and_in_a_graph(engine):
     sa = _sa()
     c = _case(89, 3, 6, 32, 8, [3000, 40, 700], [2500, 40, 333], tail=6)
-    ref = _run(c)
+    ref = _run(c, engine=engine)
     up = lambda t: t.to(DEV)
     q, codes, params, table, idx, counts = up(c["q"]), _to_gpu(c["codes"]), _to_gpu(c["params"]), up(c["table"]), up(c["idx"]), up(c["counts"])
     lens = torch.tensor(c["lens"], dtype=torch.int32, device=DEV)
-    kw = dict(block_table=table, idx=idx, counts=counts, tail_len=6)
+    kw = dict(block_table=table, idx=idx, counts=counts, tail_len=6, flags=ENGINES[engine])
     torch.cuda.synchronize()
     streams = [torch.cuda.Stream() for _ in range(2)]
     got = []
@@ -430,5 +478,6 @@ def test_random_shapes(seed):
     counts = [int(x * float(torch.rand(1, generator=r))) for x in lens]
     c = _case(seed, B, T, Hq, Hkv, lens, counts, page=pick(16, 32, 64, 7, 1), dtype=pick(torch.bfloat16, torch.float16),
               layout=pick("head", "slot"), G=pick(1, Hkv) if not dense else 1, tail=pick(0, T, T + 2, 1), dense=dense, paged=pick(True, False))
-    out, lse, _ = _run(c)
-    _check(c, out, lse)
+    for engine in _engines(T, Hq, Hkv):
+        out, lse, _ = _run(c, engine)
+        _check(c, out, lse)
