@@ -500,8 +500,7 @@ int specattn_kv4_read(const specattn_kv4_rows_args* args, void* cuda_stream);
  * Requirements: head_dim == 128; n_q * (n_q_heads / n_kv_heads) <= 64; batch * n_kv_heads <= 2048; lists
  * and, where dense, block_table_stride * page_size of at most 2^23 positions.
  * flags: SPECATTN_VERIFY_ENGINE_MMA_SYNC or SPECATTN_VERIFY_ENGINE_TCGEN05 forces one of two implementations of the same
- * operation; TCGEN05 needs 17 query rows or more (else SPECATTN_ERR_UNSUPPORTED).  With neither the kernel itself picks by
- * the lengths that it finds: tcgen05 for 17 rows and more where the lists are long enough to fill the GPU.  Results
+ * operation.  With neither the kernel itself picks by the lengths that it finds: tcgen05 where they fill the GPU.  Results
  * agree within the tolerance of the operation either way.
  * workspace: specattn_kv4_verify_workspace_bytes() bytes, 256-byte aligned, no preparation and no
  * state between calls; two calls that may overlap on the GPU need separate ones.

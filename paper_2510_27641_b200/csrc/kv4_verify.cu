@@ -33,22 +33,26 @@ int device_sm_count();
 
 namespace {
 
-// What a call of R8 * 8 query rows runs with.
+constexpr int kThreads = 512;
+
+// What a call of R8 * 8 query rows runs with on mma.sync.
 template <int R8>
 struct Config {
-  static constexpr int kGroups = R8 > 4 ? 2 : 1;               // of query rows, on mma.sync: 32 are as many as registers hold
+  static constexpr int kGroups = R8 > 4 ? 2 : 1;               // of query rows: 32 are as many as registers hold
   static constexpr int kTiles = (R8 + kGroups - 1) / kGroups;  // of eight queries
-  static constexpr int kWarps = R8 == 1 ? 16 : R8 == 2 ? 12 : 8;
-  static constexpr int kStages = R8 <= 2 ? 3 : 4;
-  static constexpr bool kTensor = R8 >= 3;
+  // Sixteen warps while 128 registers hold a warp's output; else eight take the registers of the others.
+  static constexpr int kWarps = R8 == 1 ? 16 : 8;
+  static constexpr int kStages = R8 == 1 ? 3 : 4;
   using Mma = MmaPath<kTiles, kWarps, kStages>;
-  static constexpr int kSmem = kTensor && kTcSmem > Mma::kSmem ? kTcSmem : Mma::kSmem;
+  static constexpr int kSmem = kTcSmem > Mma::kSmem ? kTcSmem : Mma::kSmem;
 };
+constexpr int kLaunchRegisters = 128, kMoreRegisters = 232, kFewRegisters = 24;
+static_assert(kMoreRegisters + kFewRegisters == 2 * kLaunchRegisters, "eight warps give what eight take");
 
 constexpr int kTensorLeast = 64;  // chunks of 32 positions to a CTA from which on tcgen05 is ahead
 
 template <int R8>
-__global__ void __launch_bounds__(Config<R8>::kWarps * 32, 1) kv4_verify_kernel(const __grid_constant__ Kv4Params P) {
+__global__ void __launch_bounds__(kThreads, 1) kv4_verify_kernel(const __grid_constant__ Kv4Params P) {
   using C = Config<R8>;
   extern __shared__ __align__(1024) unsigned char smem[];
   __shared__ PartitionShared ps;
@@ -58,23 +62,29 @@ __global__ void __launch_bounds__(Config<R8>::kWarps * 32, 1) kv4_verify_kernel(
     __device__ Shared() {}
   } sh;
   pdl_wait();  // everything below reads what earlier kernels may have written
-  int before;
-  int total = count_chunks<C::kWarps * 32>(P, units_of(P, 0).n, kChunk, ps, &before);
-  if constexpr (C::kTensor) {
-    if (P.engine == 2 || (P.engine == 0 && total / P.groups_of_rows >= kTensorLeast * static_cast<int>(gridDim.x))) {
-      __syncthreads();
-      const int units = units_of(P, 1).n;
-      total = count_chunks<C::kWarps * 32>(P, units, kTile, ps, &before);
-      if (threadIdx.x == 0) sh.tc.bad[0] = sh.tc.bad[1] = 0;
-      const Partition part = cut<C::kWarps * 32>(P, units, kTile, 2, 1, ps, total, before);
-      tc_path<R8>(P, part, smem, sh.tc);
-      pdl_launch_dependents();
-      return;
-    }
+  bool tensor = P.engine == 2;
+  if (P.engine == 0) {
+    const int units = units_of(P, 1).n;
+    int mine = 0, total;
+    for (int u = threadIdx.x; u < units; u += kThreads) mine += chunks_of(P, u, kChunk);
+    scan<kThreads>(mine, ps, &total);
+    tensor = total >= kTensorLeast * static_cast<int>(gridDim.x);
   }
-  if (threadIdx.x == 0) sh.mma.bad[0] = sh.mma.bad[1] = 0;
-  const Partition part = cut<C::kWarps * 32>(P, units_of(P, 0).n, kChunk, C::kWarps, 0, ps, total, before);
-  mma_path<C::kTiles, C::kWarps, C::kStages>(P, part, smem, sh.mma);
+  if (tensor) {
+    const Partition part = cut<kThreads>(P, 1, kTile, 2, 12, ps);
+    tc_path<R8>(P, part, smem, sh.tc);
+  } else {
+    if (threadIdx.x < 2) sh.mma.bad[threadIdx.x] = sh.mma.qmax[threadIdx.x] = 0;
+    const Partition part = cut<kThreads>(P, 0, kChunk, C::kWarps, 32, ps);
+    if constexpr (C::kWarps * 32 < kThreads) {
+      if (threadIdx.x >= C::kWarps * 32) {
+        set_max_registers_dec<kFewRegisters>();
+        return;
+      }
+      set_max_registers_inc<kMoreRegisters>();
+    }
+    mma_path<C::kTiles, C::kWarps, C::kStages>(P, part, smem, sh.mma);
+  }
   pdl_launch_dependents();
 }
 
@@ -82,8 +92,7 @@ __global__ void __launch_bounds__(Config<R8>::kWarps * 32, 1) kv4_verify_kernel(
 __global__ void __launch_bounds__(256) kv4_join_kernel(const __grid_constant__ Kv4Params P) {
   pdl_launch_dependents();
   pdl_wait();
-  const int per = P.starts[P.most_units + 1];
-  const Units units = units_of(P, P.starts[P.most_units + 2]);
+  const Units units = units_of(P, *P.path);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const long long rec_floats = static_cast<long long>(units.rows) * kRowFloats;
   // (the part of the CTA where a unit begins is that CTA's second record, all others are first records)
@@ -93,14 +102,11 @@ __global__ void __launch_bounds__(256) kv4_join_kernel(const __grid_constant__ K
     for (int b = warp; b < P.B; b += 8) {
       int flag = 0;
       for (int i = lane; i < units.n / P.B; i += 32) {
-        const int u = (i / P.H) * P.B * P.H + b * P.H + i % P.H, c0 = P.starts[u], c1 = P.starts[u + 1];
-        if (c0 == c1) continue;
-        const int first = c0 / per, last = (c1 - 1) / per;
-        if (first == last) {
-          flag |= P.flags[u];
-        } else {
-          for (int c = first; c <= last; ++c) flag |= __float_as_int(rec_of(c, first)[kKv4D + 2]);
-        }
+        const int u = (i / P.H) * P.B * P.H + b * P.H + i % P.H;
+        const int2 of = P.parts[u];
+        if (of.x == of.y) flag |= P.flags[u];
+        if (of.x < of.y)
+          for (int c = of.x; c <= of.y; ++c) flag |= __float_as_int(rec_of(c, of.x)[kKv4D + 2]);
       }
       flag = __reduce_or_sync(0xffffffffu, flag);
       if (lane == 0) P.status[b] = flag;
@@ -109,26 +115,36 @@ __global__ void __launch_bounds__(256) kv4_join_kernel(const __grid_constant__ K
   }
   const int u = blockIdx.x;
   if (u >= units.n) return;
-  const int c0 = P.starts[u], c1 = P.starts[u + 1];
-  const int first = c0 / per, last = c1 > c0 ? (c1 - 1) / per : first;
-  if (c1 > c0 && first == last) return;
+  const int2 of = P.parts[u];
+  if (of.x == of.y) return;
   const int rg = u / (P.B * P.H), bh = u - rg * P.B * P.H, b = bh / P.H, h = bh - b * P.H;
   const int row0 = rg * units.rows, r = blockIdx.y * 8 + warp;
   if (r >= min(units.rows, P.rows - row0)) return;
   float m = -FLT_MAX, l = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (c1 > c0) {
-    for (int c = first + lane; c <= last; c += 32) m = fmaxf(m, rec_of(c, first)[r * kRowFloats + kKv4D]);
+  // four parts at a time, from a maximum that moves with them
+  for (int c0 = of.x; c0 <= of.y; c0 += 4) {
+    float2 ml[4];
+    float4 x[4];
 #pragma unroll
-    for (int s = 16; s > 0; s >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, s));
-#pragma unroll 4
-    for (int c = first; c <= last; ++c) {
-      const float* rec = rec_of(c, first) + r * kRowFloats;
-      const float2 ml = *reinterpret_cast<const float2*>(rec + kKv4D);
-      const float4 x = *reinterpret_cast<const float4*>(rec + 4 * lane);
-      const float f = ex2(ml.x - m);
-      l = fmaf(f, ml.y, l);
-      o.x = fmaf(f, x.x, o.x), o.y = fmaf(f, x.y, o.y), o.z = fmaf(f, x.z, o.z), o.w = fmaf(f, x.w, o.w);
+    for (int j = 0; j < 4; ++j) {
+      ml[j] = make_float2(-FLT_MAX, 0.f);
+      x[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (c0 + j <= of.y) {
+        const float* rec = rec_of(c0 + j, of.x) + r * kRowFloats;
+        ml[j] = *reinterpret_cast<const float2*>(rec + kKv4D);
+        x[j] = *reinterpret_cast<const float4*>(rec + 4 * lane);
+      }
+    }
+    const float top = fmaxf(m, fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x))), back = ex2(m - top);
+    m = top;
+    l *= back;
+    o.x *= back, o.y *= back, o.z *= back, o.w *= back;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float f = ex2(ml[j].x - m);
+      l = fmaf(f, ml[j].y, l);
+      o.x = fmaf(f, x[j].x, o.x), o.y = fmaf(f, x[j].y, o.y), o.z = fmaf(f, x[j].z, o.z), o.w = fmaf(f, x[j].w, o.w);
     }
   }
   write_row(P, b, h, row0 + r, lane, o, m, l);
@@ -152,16 +168,15 @@ int validate(const specattn_kv4_verify_args* args) {
   if (A.head_dim != kKv4D || A.n_q > SPECATTN_MAX_QUERY_ROWS || A.n_q * (A.n_q_heads / A.n_kv_heads) > SPECATTN_MAX_QUERY_ROWS ||
       static_cast<long long>(A.batch) * A.n_kv_heads > kMaxUnits)
     return SPECATTN_ERR_UNSUPPORTED;
-  if ((A.flags & SPECATTN_VERIFY_ENGINE_TCGEN05) && A.n_q * (A.n_q_heads / A.n_kv_heads) <= 16) return SPECATTN_ERR_UNSUPPORTED;
   return SPECATTN_OK;
 }
 
-// starts, the run's length and the path, flags; then the records
-size_t starts_bytes(const specattn_kv4_verify_args& A) {
-  return (static_cast<size_t>(A.batch) * A.n_kv_heads * groups_of(query_tiles(A)) * 2 + 3 + 63) / 64 * 256;
+// the path, parts, flags; then the records
+size_t table_bytes(const specattn_kv4_verify_args& A) {
+  return (static_cast<size_t>(A.batch) * A.n_kv_heads * groups_of(query_tiles(A)) * 3 + 2 + 63) / 64 * 256;
 }
 size_t workspace_bytes(const specattn_kv4_verify_args& A, int sms) {
-  return starts_bytes(A) + static_cast<size_t>(2) * sms * query_tiles(A) * 8 * kRowFloats * sizeof(float);
+  return table_bytes(A) + static_cast<size_t>(2) * sms * query_tiles(A) * 8 * kRowFloats * sizeof(float);
 }
 
 template <int R8>
@@ -174,7 +189,10 @@ int launch(const Kv4Params& P, int sms, cudaStream_t stream) {
     return SPECATTN_ERR_CUDA;
   }
   if (!((prepared.load(std::memory_order_acquire) >> dev) & 1ull)) {
-    if (cudaFuncSetAttribute(kv4_verify_kernel<R8>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem) != cudaSuccess) {
+    // (what one half of the warps gives the other takes: with fewer registers at launch they would wait for ever)
+    cudaFuncAttributes built;
+    if (cudaFuncGetAttributes(&built, kv4_verify_kernel<R8>) != cudaSuccess || built.numRegs != kLaunchRegisters ||
+        cudaFuncSetAttribute(kv4_verify_kernel<R8>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem) != cudaSuccess) {
       cudaGetLastError();
       return SPECATTN_ERR_CUDA;
     }
@@ -183,7 +201,7 @@ int launch(const Kv4Params& P, int sms, cudaStream_t stream) {
   cudaLaunchConfig_t cfg;
   memset(&cfg, 0, sizeof(cfg));
   cfg.gridDim = dim3(sms);
-  cfg.blockDim = dim3(C::kWarps * 32);
+  cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = C::kSmem;
   cfg.stream = stream;
   cudaLaunchAttribute attr[1];
@@ -250,9 +268,10 @@ extern "C" int specattn_kv4_verify(const specattn_kv4_verify_args* args, void* c
   P.lse = A.lse;
   P.status = A.status;
   P.most_units = A.batch * A.n_kv_heads * groups;
-  P.starts = static_cast<int*>(A.workspace);
-  P.flags = P.starts + P.most_units + 3;
-  P.partial = reinterpret_cast<float*>(static_cast<unsigned char*>(A.workspace) + starts_bytes(A));
+  P.path = static_cast<int*>(A.workspace);
+  P.parts = reinterpret_cast<int2*>(P.path + 2);
+  P.flags = P.path + 2 + 2 * P.most_units;
+  P.partial = reinterpret_cast<float*>(static_cast<unsigned char*>(A.workspace) + table_bytes(A));
   P.scale = (A.sm_scale != 0.f ? A.sm_scale : 1.0f / sqrtf(static_cast<float>(A.head_dim))) * kLog2e;
   P.B = A.batch;
   P.T = A.n_q;

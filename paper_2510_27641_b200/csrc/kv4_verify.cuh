@@ -26,7 +26,8 @@ struct Kv4Params {
   unsigned char* out;
   float* lse;
   int* status;
-  int* starts;     // workspace: first chunk of every unit, [units + 1], chunks of a CTA, the path taken
+  int* path;       // workspace: the path taken
+  int2* parts;     // workspace: first and last CTA of every unit, (0, -1) where it has no positions
   int* flags;      // workspace: status of the units that one CTA has done, [units]; other units have it in their records
   float* partial;  // workspace: two records of a unit's rows for every CTA
   float scale;     // sm_scale * log2(e)
@@ -83,26 +84,25 @@ __device__ __forceinline__ int chunks_of(const Kv4Params& P, int u, int chunk) {
 
 struct PartitionShared {
   int scan[33];
-  int unit, unit_start, total;
+  int unit, unit_start, total, length;
 };
-// Chunks of `chunk` positions of all units in a row, cut into equal runs: this CTA's is [first, last), its first unit
-// `unit` begins at chunk `start`.
+// The units' chunks of `chunk` positions in a row, cut: this CTA's run is [first, last), its first unit `unit` begins
+// at chunk `start`.
 struct Partition {
-  int total, per, first, last, unit, start;
+  int first, last, unit, start;
 };
+
+// The exclusive prefix of v over the threads of the CTA; the total in *total.
 template <int kThreads>
-__device__ __forceinline__ int count_chunks(const Kv4Params& P, int units, int chunk, PartitionShared& S, int* before) {
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int per_thread = (units + kThreads - 1) / kThreads;
-  const int u0 = min(tid * per_thread, units), u1 = min(u0 + per_thread, units);
-  int sum = 0;
-  for (int u = u0; u < u1; ++u) sum += chunks_of(P, u, chunk);
-  int incl = sum;
+__device__ __forceinline__ int scan(int v, PartitionShared& S, int* total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int incl = v;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
     const int y = __shfl_up_sync(0xffffffffu, incl, o);
     if (lane >= o) incl += y;
   }
+  __syncthreads();  // the last scan's sums have been read
   if (lane == 31) S.scan[warp] = incl;
   __syncthreads();
   if (warp == 0) {
@@ -114,35 +114,73 @@ __device__ __forceinline__ int count_chunks(const Kv4Params& P, int units, int c
       if (lane >= o) y += z;
     }
     if (lane < kThreads / 32) S.scan[lane] = y - x;
-    if (lane == 31) S.total = y;
-    if (lane == 0) S.unit = units, S.unit_start = 0;
+    if (lane == 31) S.scan[32] = y;
   }
   __syncthreads();
-  *before = S.scan[warp] + incl - sum;
-  return S.total;
+  *total = S.scan[32];
+  return S.scan[warp] + incl - v;
 }
+
+// Two ways to cut.  Equal runs of all chunks, wherever units begin and end: every CTA does the same work, but one that meets
+// the end of a unit pays for the start of the next (`afresh`: as many chunks as take as long).  Or, where there are CTAs
+// enough, equal parts of units: the shortest length for which the parts are no more than the CTAs is searched for, and
+// taken if it exceeds an equal run by less than that.
 template <int kThreads>
-__device__ __forceinline__ Partition cut(const Kv4Params& P, int units, int chunk, int least, int tensor, PartitionShared& S, int total, int before) {
-  Partition p;
-  const int tid = threadIdx.x;
-  p.total = total;
-  p.per = max((total + static_cast<int>(gridDim.x) - 1) / static_cast<int>(gridDim.x), least);
-  p.first = min(static_cast<long long>(blockIdx.x) * p.per, static_cast<long long>(total));
-  p.last = min(p.first + p.per, total);
+__device__ __forceinline__ Partition cut(const Kv4Params& P, int tensor, int chunk, int least, int afresh, PartitionShared& S) {
+  const int tid = threadIdx.x, grid = static_cast<int>(gridDim.x), units = units_of(P, tensor).n;
   const int per_thread = (units + kThreads - 1) / kThreads;
   const int u0 = min(tid * per_thread, units), u1 = min(u0 + per_thread, units);
+  int mine = 0, total;
+  for (int u = u0; u < u1; ++u) mine += chunks_of(P, u, chunk);
+  const int before = scan<kThreads>(mine, S, &total);
+  Partition p;
+  p.unit = units;
+  p.start = p.first = p.last = 0;
+  const int per = max((total + grid - 1) / grid, least);
+  if (tid == 0) S.unit = units;
+  __syncthreads();
+  if (units <= grid && units <= kThreads) {  // (a unit to a thread)
+    // parts of at most `length` chunks, the length doubled in quarters until they fit
+    int length = per, count = 0, k = 0;
+    for (int step = 0; step < 32; ++step) {
+      k = (mine + length - 1) / length;
+      int all;
+      const int at = scan<kThreads>(k, S, &all);
+      if (all <= grid || length - per >= afresh) {
+        if (all > grid) break;
+        count = all;
+        // this thread's unit goes to CTAs at ... at + k - 1
+        if (tid < units) {
+          if (blockIdx.x == 0) P.parts[tid] = make_int2(k > 0 ? at : 0, at + k - 1 - (k > 0 ? 0 : at));
+          const int j = static_cast<int>(blockIdx.x) - at;
+          if (j >= 0 && j < k) {
+            S.unit = tid;
+            S.unit_start = before;
+            S.total = before + static_cast<int>(static_cast<long long>(mine) * j / k);
+            S.length = before + static_cast<int>(static_cast<long long>(mine) * (j + 1) / k);
+          }
+        }
+        break;
+      }
+      length += max(1, length / 8);
+    }
+    __syncthreads();
+    if (count > 0 || total == 0) {
+      if (S.unit < units) p.unit = S.unit, p.start = S.unit_start, p.first = S.total, p.last = S.length;
+      if (blockIdx.x == 0 && tid == 0) *P.path = tensor;
+      return p;
+    }
+  }
+  p.first = static_cast<int>(min(static_cast<long long>(blockIdx.x) * per, static_cast<long long>(total)));
+  p.last = min(p.first + per, total);
   int run = before;
   for (int u = u0; u < u1; ++u) {
     const int n = chunks_of(P, u, chunk);
-    if (blockIdx.x == 0) P.starts[u] = run;
+    if (blockIdx.x == 0) P.parts[u] = n > 0 ? make_int2(run / per, (run + n - 1) / per) : make_int2(0, -1);
     if (n > 0 && run <= p.first && p.first < run + n) S.unit = u, S.unit_start = run;
     run += n;
   }
-  if (blockIdx.x == 0 && tid == 0) {
-    P.starts[units] = total;
-    P.starts[P.most_units + 1] = p.per;
-    P.starts[P.most_units + 2] = tensor;
-  }
+  if (blockIdx.x == 0 && tid == 0) *P.path = tensor;
   __syncthreads();
   p.unit = S.unit;
   p.start = S.unit_start;
@@ -175,83 +213,87 @@ struct Gather {
     }
     return -2;
   }
-  // A lane's position and page; the warp copies the 32 rows to a stage: K rows, V rows, then (s, z, t, y) of each.
-  // `place_k` and `place_v`: where 16-byte piece t of row r goes, from the rows' beginning.
-  template <typename PlaceK, typename PlaceV>
-  __device__ __forceinline__ void fetch(uint32_t stage, int pos, int pg, int lane, int* bad, PlaceK place_k, PlaceV place_v) const {
-    long long off = 0;
-    int bytes = 0;
-    const unsigned char* par = P.cache.params;
-    if (pos != -1) {
-      int slot = 0;
-      if (pg < 0) {  // position 0 / page 0 in its place
-        *bad = SPECATTN_ROW_BAD_INDEX;
-        pg = 0;
-      } else {
-        slot = pos - pos / P.cache.by_page * P.cache.page_size;
-      }
-      off = pg * P.cache.s_page + slot * P.cache.s_slot + h * P.cache.s_head;
-      par += pg * P.cache.p_page + slot * P.cache.p_slot + h * P.cache.p_head;
-      bytes = 4;
+  // Where a row lies: bytes from the codes' and the params' beginning; position 0 / page 0 where a position or page is
+  // out of range.
+  __device__ __forceinline__ long long locate(int pos, int pg, int* bad, long long* params) const {
+    *params = 0;
+    if (pos == -1) return 0;
+    int slot = 0;
+    if (pg < 0) {
+      *bad = SPECATTN_ROW_BAD_INDEX;
+      pg = 0;
+    } else {
+      slot = pos - pos / P.cache.by_page * P.cache.page_size;
     }
-    // (a position that is none leaves zeros for scale and zero point, and any codes)
-    cp_async4(stage + 2 * kChunk * kKv4Row + lane * 8, par, bytes);
-    cp_async4(stage + 2 * kChunk * kKv4Row + lane * 8 + 4, par + P.cache.p_kv, bytes);
-    const int t = lane & 3;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int row = j * 8 + (lane >> 2);
-      const long long o = __shfl_sync(0xffffffffu, off, row);
-      const unsigned char* from = P.cache.codes + o + t * 16;
-      cp_async16(stage + place_k(row, t), from);
-      cp_async16(stage + kChunk * kKv4Row + place_v(row, t), from + P.cache.s_kv);
-    }
+    *params = pg * P.cache.p_page + slot * P.cache.p_slot + h * P.cache.p_head;
+    return pg * P.cache.s_page + slot * P.cache.s_slot + h * P.cache.s_head;
   }
 };
 
-// Query rows of a unit: byte offsets, what they see of the tail, their sums; and the power of two that takes the largest
-// finite |q| to [2^14, 2^15): all 8 (or 11) bits of what lies within 2^-28 of it stay in fp16.
+// A query row's first element.
 __device__ __forceinline__ long long query_at(const Kv4Params& P, int b, int h, int row) {
   const int tok = row / P.grp, hq = h * P.grp + row - tok * P.grp;
   return ((static_cast<long long>(b) * P.T + tok) * P.Hq + hq) * kKv4D;
 }
+
+// The query rows of a unit as fp16 operands: a warp has every kWarps-th row, a lane four elements of it.  load() asks for
+// them; look() finds sums, what the rows see of the tail, and the largest finite |q|; and, behind a barrier, place() writes
+// them, scaled by the power of two that takes that largest to [2^14, 2^15): all 8 (or 11) bits of what lies within 2^-28
+// of it stay.  Against a word of codes go pairs of elements (0, 4), (1, 5) from an even lane and (2, 6), (3, 7) from
+// an odd one; the second of each meets the high codes of a byte and carries 2^-4.
 template <int kWarps, int kQueries>
-__device__ __forceinline__ void look_at_queries(const Kv4Params& P, int b, int h, int row0, int n_rows, int* qmax, float* qsum, int* limit) {
-  const int lane = threadIdx.x & 31;
-  for (int r = threadIdx.x >> 5; r < kQueries; r += kWarps) {
-    float amax = 0.f, qs = 0.f;
-    if (r < n_rows) {
-      const uint2 x = *reinterpret_cast<const uint2*>(P.q + query_at(P, b, h, row0 + r) * 2 + lane * 8);
-      const float2 a = widen16(x.x, P.half), c = widen16(x.y, P.half);
-      qs = (a.x + a.y) + (c.x + c.y);
+struct Queries {
+  static constexpr int kMine = (kQueries + kWarps - 1) / kWarps;
+  uint2 x[kMine];
+
+  __device__ __forceinline__ void load(const Kv4Params& P, int b, int h, int row0, int n_rows) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+      const int r = warp + i * kWarps;
+      x[i] = r < n_rows ? *reinterpret_cast<const uint2*>(P.q + query_at(P, b, h, row0 + r) * 2 + lane * 8) : make_uint2(0u, 0u);
+    }
+  }
+  __device__ __forceinline__ void look(const Kv4Params& P, int row0, int n_rows, int* qmax, float* qsum, int* limit) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    float most = 0.f;
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+      const int r = warp + i * kWarps;
+      const float2 a = widen16(x[i].x, P.half), c = widen16(x[i].y, P.half);
+      float qs = (a.x + a.y) + (c.x + c.y);
       const float v[4] = {fabsf(a.x), fabsf(a.y), fabsf(c.x), fabsf(c.y)};
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        if (v[e] <= FLT_MAX) amax = fmaxf(amax, v[e]);
-    }
+        if (v[e] <= FLT_MAX) most = fmaxf(most, v[e]);
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-      qs += __shfl_xor_sync(0xffffffffu, qs, o);
+      for (int o = 16; o > 0; o >>= 1) qs += __shfl_xor_sync(0xffffffffu, qs, o);
+      if (lane == 0 && r < kQueries) {
+        qsum[r] = qs * P.scale;
+        const int tok = r < n_rows ? (row0 + r) / P.grp : 0;
+        limit[r] = max(0, min(P.tail, tok + P.tail - P.T + 1));
+      }
     }
-    if (lane == 0) {
-      qsum[r] = r < n_rows ? qs * P.scale : 0.f;
-      const int tok = r < n_rows ? (row0 + r) / P.grp : 0;
-      limit[r] = max(0, min(P.tail, tok + P.tail - P.T + 1));
-      atomicMax(qmax, __float_as_int(amax));
+    const int top = __reduce_max_sync(0xffffffffu, __float_as_int(most));  // (bits of a number that is not negative)
+    if (lane == 0) atomicMax(qmax, top);
+  }
+  // to(row, word, half, operand): word 0..15 of eight elements, its half of two registers
+  template <typename To>
+  __device__ __forceinline__ void place(const Kv4Params& P, float up, To to) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const float hi = up * 0.0625f;
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+      const int r = warp + i * kWarps;
+      const bool odd = lane & 1;
+      const uint32_t other = __shfl_xor_sync(0xffffffffu, odd ? x[i].x : x[i].y, 1);
+      const float2 a = widen16(odd ? other : x[i].x, P.half), c = widen16(odd ? x[i].y : other, P.half);
+      if (r < kQueries) to(r, lane >> 1, lane & 1, make_uint2(pack_f16(a.x * up, c.x * up), pack_f16(a.y * hi, c.y * hi)));
     }
   }
-}
+};
 __device__ __forceinline__ int query_exponent(int qmax) {
   return min(14 - ((qmax >> 23) - 127), 120);  // (qmax is 0 or the bits of a positive number)
-}
-// Two 16-byte halves of eight neighbouring elements d ... d + 7 of a query row as fp16 operands against a word of codes:
-// pairs (0, 4), (1, 5), (2, 6), (3, 7); what meets the high codes of a byte carries 2^-4.
-__device__ __forceinline__ uint4 query_word(const Kv4Params& P, long long at, float up) {
-  const uint4 x = *reinterpret_cast<const uint4*>(P.q + at * 2);
-  const float2 a = widen16(x.x, P.half), b = widen16(x.y, P.half), c = widen16(x.z, P.half), d = widen16(x.w, P.half);
-  const float hi = up * 0.0625f;
-  return make_uint4(pack_f16(a.x * up, c.x * up), pack_f16(a.y * hi, c.y * hi), pack_f16(b.x * up, d.x * up), pack_f16(b.y * hi, d.y * hi));
 }
 
 // out and lse of a query row from its unnormalised output (four elements a lane), maximum and sum.

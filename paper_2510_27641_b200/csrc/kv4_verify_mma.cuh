@@ -44,8 +44,7 @@ struct MmaPath {
 
 template <int kQueries>
 struct MmaShared {
-  int bad[2];  // of this segment, and cleared for the next
-  int qmax;
+  int bad[2], qmax[2];  // of this segment, and cleared for the next
   float qsum[kQueries];  // times the scale
   int limit[kQueries];   // how many tail positions a query row sees
 };
@@ -57,6 +56,7 @@ __device__ __forceinline__ void mma_path(const Kv4Params& P, const Partition& pa
   const int g = lane >> 2, t = lane & 3;
   const uint32_t ring_at = smem_u32(smem + K::kQBytes + warp * K::kRing);
   const Units units = units_of(P, 0);
+  const auto sync = [] { named_bar_sync(5, NWARP * 32); };  // (other warps of the CTA may have left)
   int u = part.unit, u_start = part.start, turn = 0;
 
   // ---- one segment of a unit after the other ----
@@ -68,17 +68,27 @@ __device__ __forceinline__ void mma_path(const Kv4Params& P, const Partition& pa
     const int row0 = rg * units.rows, n_rows = min(units.rows, P.rows - row0);
 
     auto position = [&](int chunk) { return chunk < seg1 ? G.position(chunk * kChunk + lane) : -1; };
+    // The warp copies its 32 rows to a stage: K rows, V rows, then (s, z, t, y) of each.
     auto fetch = [&](int chunk, int pos, int pg) {
-      // K rows lie in order.  Row j of a V tile of 16 lies where the second product's lanes find it without bank
-      // conflicts: 2 t -> t, 2 t + 1 -> t + 4 within eight, its 32-byte halves swapped by bit 1.
-      G.fetch(ring_at + ((chunk / NWARP) % STAGES) * kStageBytes, pos, pg, lane, &S.bad[turn],
-              [](int row, int piece) { return row * kKv4Row + piece * 16; },
-              [](int row, int piece) {
-                const int r8 = row & 7, at_row = (row & ~7) | ((r8 >> 1) | ((r8 & 1) << 2));
-                return at_row * kKv4Row + ((piece * 16) ^ ((at_row & 2) << 4));
-              });
+      const uint32_t stage = ring_at + ((chunk / NWARP) % STAGES) * kStageBytes;
+      long long par;
+      const long long off = G.locate(pos, pg, &S.bad[turn], &par);
+      const int bytes = pos != -1 ? 4 : 0;  // (a position that is none leaves zeros for scale and zero point, and any codes)
+      cp_async4(stage + 2 * kChunk * kKv4Row + lane * 8, P.cache.params + par, bytes);
+      cp_async4(stage + 2 * kChunk * kKv4Row + lane * 8 + 4, P.cache.params + par + P.cache.p_kv, bytes);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        // four lanes a row.  K rows lie in order.  Row j of a V tile of 16 lies where the second product's lanes find
+        // it without bank conflicts: 2 t -> t, 2 t + 1 -> t + 4 within eight, its 32-byte halves swapped by bit 1.
+        const int row = j * 8 + g, r8 = row & 7, v_row = (row & ~7) | ((r8 >> 1) | ((r8 & 1) << 2));
+        const unsigned char* from = P.cache.codes + __shfl_sync(0xffffffffu, off, row) + t * 16;
+        cp_async16(stage + row * kKv4Row + t * 16, from);
+        cp_async16(stage + (kChunk + v_row) * kKv4Row + ((t * 16) ^ ((v_row & 2) << 4)), from + P.cache.s_kv);
+      }
     };
 
+    Queries<NWARP, K::kQueries> queries;
+    queries.load(P, b, h, row0, n_rows);
     // the first chunks are on their way before the queries are read
     const int first = seg0 + ((warp - seg0) % NWARP + NWARP) % NWARP;  // this warp's: chunk % NWARP == warp
     int pos_next, pg_next, pos_then;  // of chunk + (STAGES - 1) NWARP; of the one behind it
@@ -99,24 +109,16 @@ __device__ __forceinline__ void mma_path(const Kv4Params& P, const Partition& pa
     }
 
     // ---- queries ----
-    if (tid == 0) S.qmax = 0;
-    __syncthreads();
-    if (tid == 0) S.bad[turn ^ 1] = 0;
-    look_at_queries<NWARP, K::kQueries>(P, b, h, row0, n_rows, &S.qmax, S.qsum, S.limit);
-    __syncthreads();
-    const int qexp = query_exponent(S.qmax);
-    const float q_up = __int_as_float((127 + qexp) << 23);
+    queries.look(P, row0, n_rows, &S.qmax[turn], S.qsum, S.limit);
+    sync();
+    if (tid == 0) S.bad[turn ^ 1] = S.qmax[turn ^ 1] = 0;
+    const int qexp = query_exponent(S.qmax[turn]);
     // step 2 w meets codes 0, 4 (low halves of bytes) and 1, 5 (high) of word w of the lane's 16 bytes, step 2 w + 1
     // codes 2, 6 and 3, 7
-    for (int i = tid; i < NT * 4 * 32; i += NWARP * 32) {
-      const int nt = i >> 7, w = (i >> 5) & 3, l = i & 31, r = nt * 8 + (l >> 2);
-      uint4 x = make_uint4(0u, 0u, 0u, 0u);
-      if (r < n_rows) x = query_word(P, query_at(P, b, h, row0 + r) + (l & 3) * 32 + w * 8, q_up);
-      uint2* to = reinterpret_cast<uint2*>(smem) + (nt * 8 + 2 * w) * 32 + l;
-      to[0] = make_uint2(x.x, x.y);
-      to[32] = make_uint2(x.z, x.w);
-    }
-    __syncthreads();
+    queries.place(P, __int_as_float((127 + qexp) << 23), [&](int r, int word, int half, uint2 x) {
+      reinterpret_cast<uint2*>(smem)[((r >> 3) * 8 + 2 * (word & 3) + half) * 32 + (r & 7) * 4 + (word >> 2)] = x;
+    });
+    sync();
     const float k_mul = P.scale * 16777216.f * __int_as_float((127 - qexp) << 23);  // codes are c 2^-24 in the product
     float sq[NT][2], m[NT][2], l[NT][2], y[NT][2];  // sum q; running maximum (log2), sum of p, sum of p (y + 8 t)
     float acc[8][NT][4], acc8[NT][4];                // output by (element tile, query tile), less its middle
@@ -313,7 +315,7 @@ __device__ __forceinline__ void mma_path(const Kv4Params& P, const Partition& pa
       }
     }
     cp_wait<0>();
-    __syncthreads();  // the rings are free
+    sync();  // the rings are free
 
     // ---- the warps' parts meet ----
     float* meet = reinterpret_cast<float*>(smem + K::kQBytes);
@@ -344,7 +346,7 @@ __device__ __forceinline__ void mma_path(const Kv4Params& P, const Partition& pa
           }
         }
     }
-    __syncthreads();
+    sync();
     const bool whole = seg0 == 0 && seg1 == n_chunks;
     float* rec = P.partial + static_cast<long long>(2 * blockIdx.x + (seg0 == 0 ? 1 : 0)) * units.rows * kRowFloats;
     finish<NWARP, NWARP, K::kQueries>(P, meet, b, h, row0, n_rows, whole, rec);
@@ -355,7 +357,7 @@ __device__ __forceinline__ void mma_path(const Kv4Params& P, const Partition& pa
         rec[kKv4D + 2] = __int_as_float(S.bad[turn]);
     }
     turn ^= 1;
-    __syncthreads();  // the records have been read
+    sync();  // the records have been read
     at = u_start + seg1;
     if (seg1 == n_chunks) {
       u_start += n_chunks;

@@ -25,19 +25,20 @@ namespace specattn {
 namespace {
 
 constexpr int kTile = 128;
-constexpr int kTcWarps = 8;
+constexpr int kTcWarps = 16;
 constexpr int kTcRing = 3;
-constexpr int kTcSmem = 2 * 32768 + 2 * 16384 + 16384 + kTcWarps * kTcRing * kStageBytes + 1024;
+constexpr int kTcStage = kChunk * kKv4Row;  // half rows of K and V for 32 positions
+constexpr int kTcSmem = 2 * 32768 + 2 * 16384 + 16384 + kTcWarps * kTcRing * kTcStage + 1024;
 
 struct Tc4Shared {
   alignas(8) unsigned long long s_bar[2], o_bar[2];
   alignas(16) float2 base[2][64];  // (sum q, minus the running maximum) of a group's queries
   float red[2][4][64][2];          // what the warps of a group reduce
   float t_red[2][4];
-  float sums[2][64][2];            // sum of p, sum of p (y + 8 t)
+  float sums[2][64];  // sum of p (y + 8 t)
   float qsum[64];
   int limit[64];
-  int bad[2], qmax;
+  int bad[2], qmax[2];  // of this segment, and cleared for the next
   uint32_t tmem;
   volatile int abort;
 };
@@ -75,20 +76,15 @@ __device__ __forceinline__ void mma_done(unsigned long long* bar) {
 __device__ __forceinline__ void tm_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tm_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 // (the values pass through, so that nothing that uses them moves ahead of the wait)
-__device__ __forceinline__ void tm_wait_ld8(float* r) {
-  asm volatile("tcgen05.wait::ld.sync.aligned;"
-               : "+f"(r[0]), "+f"(r[1]), "+f"(r[2]), "+f"(r[3]), "+f"(r[4]), "+f"(r[5]), "+f"(r[6]), "+f"(r[7])::"memory");
+__device__ __forceinline__ void tm_wait_ld4(float* r) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;" : "+f"(r[0]), "+f"(r[1]), "+f"(r[2]), "+f"(r[3])::"memory");
 }
 __device__ __forceinline__ void tm_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void tm_ld8(float* r, uint32_t at) {
-  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-               : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7])
-               : "r"(at));
+__device__ __forceinline__ void tm_ld4(float* r, uint32_t at) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0,%1,%2,%3}, [%4];" : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]) : "r"(at));
 }
-__device__ __forceinline__ void tm_st8(uint32_t at, const float* r) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(at), "f"(r[0]), "f"(r[1]),
-               "f"(r[2]), "f"(r[3]), "f"(r[4]), "f"(r[5]), "f"(r[6]), "f"(r[7])
-               : "memory");
+__device__ __forceinline__ void tm_st4(uint32_t at, const float* r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "f"(r[0]), "f"(r[1]), "f"(r[2]), "f"(r[3]) : "memory");
 }
 __device__ __forceinline__ void tm_st16(uint32_t at, const uint32_t (&r)[16]) {
   asm volatile(
@@ -100,19 +96,20 @@ __device__ __forceinline__ void tm_st16(uint32_t at, const uint32_t (&r)[16]) {
 __device__ __forceinline__ void sts128(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
+__device__ __forceinline__ void sts64(uint32_t at, uint32_t a, uint32_t b) {
+  asm volatile("st.shared.v2.b32 [%0], {%1,%2};" ::"r"(at), "r"(a), "r"(b) : "memory");
+}
 __device__ __forceinline__ uint32_t minus(uint32_t a, uint32_t b) {
   const __half2 v = __hsub2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
   return *reinterpret_cast<const uint32_t*>(&v);
 }
 
-// The 32 lanes' values of eight columns, reduced: lane l gets column l & 7's.
+// The 32 lanes' values of four columns, reduced: lane l gets column l & 3's.
 template <typename Op>
-__device__ __forceinline__ float of_eight(const float* in, int lane, Op op) {
-  float x[8];
+__device__ __forceinline__ float of_four(const float* in, int lane, Op op) {
+  float x[4] = {in[0], in[1], in[2], in[3]};
 #pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = in[i];
-#pragma unroll
-  for (int o = 4; o > 0; o >>= 1) {
+  for (int o = 2; o > 0; o >>= 1) {
     const bool upper = lane & o;
 #pragma unroll
     for (int i = 0; i < o; ++i) {
@@ -120,18 +117,20 @@ __device__ __forceinline__ float of_eight(const float* in, int lane, Op op) {
       x[i] = op(keep, __shfl_xor_sync(0xffffffffu, give, o));
     }
   }
-  x[0] = op(x[0], __shfl_xor_sync(0xffffffffu, x[0], 8));
-  return op(x[0], __shfl_xor_sync(0xffffffffu, x[0], 16));
+#pragma unroll
+  for (int o = 4; o < 32; o <<= 1) x[0] = op(x[0], __shfl_xor_sync(0xffffffffu, x[0], o));
+  return x[0];
 }
 
 template <int R8>
 __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& part, unsigned char* smem_raw, Tc4Shared& S) {
-  constexpr int R = R8 * 8, N = (R8 + 1) / 2 * 16;
+  constexpr int R = R8 * 8, N = (R8 + 1) / 2 * 16, CR = R / 2;  // query rows; columns of the products; a thread's columns
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int g = warp >> 2, wq = warp & 3, key = wq * 32 + lane;  // group, quarter of a tile, position of a tile = lane of tensor memory
+  // group; half of a row's codes and of the queries; quarter of a tile; position of a tile = lane of tensor memory
+  const int g = warp >> 3, half = (warp >> 2) & 1, wq = warp & 3, key = wq * 32 + lane, col0 = half * CR;
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   const uint32_t v_at = smem_u32(smem) + g * 32768, w_at = smem_u32(smem) + 65536 + g * 16384, q_at = smem_u32(smem) + 98304;
-  const uint32_t ring_at = q_at + 16384 + warp * kTcRing * kStageBytes;
+  const uint32_t ring_at = q_at + 16384 + warp * kTcRing * kTcStage;
   const Units units = units_of(P, 1);
 
   if (warp == 0) {
@@ -139,80 +138,107 @@ __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& par
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   if (tid == 0) {
-    for (int i = 0; i < 2; ++i) mbar_init(&S.s_bar[i], 1), mbar_init(&S.o_bar[i], 1);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&S.s_bar[i], 1);
+      mbar_init(&S.o_bar[i], 1);
+      S.bad[i] = S.qmax[i] = 0;
+    }
     mbar_fence_init();
     S.abort = 0;
   }
-  // (columns of W beyond the query rows stay zero)
-  for (int i = tid; i < 2048; i += kTcWarps * 32) reinterpret_cast<uint4*>(smem + 65536)[i] = make_uint4(0u, 0u, 0u, 0u);
+  // (columns of W and rows of Q beyond the query rows stay zero)
+  for (int i = tid; i < 3072; i += kTcWarps * 32) reinterpret_cast<uint4*>(smem + 65536)[i] = make_uint4(0u, 0u, 0u, 0u);
   tm_before();
   __syncthreads();
   tm_after();
   const uint32_t tm_a = S.tmem + g * 192, tm_s = tm_a + 64, tm_o = tm_a + 128, mine = static_cast<uint32_t>(wq * 32) << 16;
-  const bool elected = (tid & 127) == 0;
+  const bool elected = (tid & 255) == 0;
   uint32_t s_turn = 0, o_turn = 0;  // completions of this group's products that have been waited for
   auto wait_for = [&](unsigned long long* bar, uint32_t turn) {
     if (!mbar_wait(bar, turn & 1u, &S.abort)) S.abort = 1;
   };
-  const int piece_of = (lane >> 1) & 3;  // raw rows: pieces of 16 bytes swapped so that 8 lanes meet 8 banks' groups
+  const uint32_t swap = ((lane >> 2) & 1) << 4;  // raw half rows of 32 bytes: halves swapped so that 8 lanes meet all banks
 
   int u = part.unit, u_start = part.start, turn = 0;
-  for (int at = part.first; at < part.last;) {
-    const int b = u / P.H, h = u - b * P.H;
+  int b = 0, h = 0, seg0 = 0, seg1 = 0, n_tiles = 0, n_mine = 0, n_list = 0;
+  int pos_next = -1, pg_next = -1, pos_then = -1;  // of this group's tile i + 3, of the one behind it
+  uint2 par0, par1, par2;                          // (s, z), (t, y) of this thread's position in tiles i, i + 1, i + 2
+  auto position = [&](const Gather& G, int i) { return i < n_mine ? G.position((seg0 + g + 2 * i) * kTile + key) : -1; };
+  // the warp copies its halves of 32 rows to a stage, K then V, two lanes to a row; scales come straight
+  auto fetch = [&](const Gather& G, int i, int pos, int pg) {
+    const uint32_t stage = ring_at + (i % kTcRing) * kTcStage;
+    long long par;
+    const long long off = G.locate(pos, pg, &S.bad[turn], &par);
+    uint2 x = make_uint2(0u, 0u);
+    if (pos != -1) {
+      x.x = *reinterpret_cast<const uint32_t*>(P.cache.params + par);
+      x.y = *reinterpret_cast<const uint32_t*>(P.cache.params + par + P.cache.p_kv);
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int row = j * 16 + (lane >> 1);
+      const unsigned char* from = P.cache.codes + __shfl_sync(0xffffffffu, off, row) + half * 32 + (lane & 1) * 16;
+      const uint32_t to = stage + row * 32 + (((lane & 1) ^ ((row >> 2) & 1)) << 4);
+      cp_async16(to, from);
+      cp_async16(to + kChunk * 32, from + P.cache.s_kv);
+    }
+    return x;
+  };
+  // a segment's first tiles, asked for before the segment in front is finished
+  auto begin = [&](int at) {
+    b = u / P.H;
+    h = u - b * P.H;
     const Gather G(P, b, h);
-    const int n_list = G.n_list, n_tiles = (G.n_all + kTile - 1) / kTile;
-    const int seg0 = at - u_start, seg1 = min(n_tiles, part.last - u_start);
-    const int n_mine = max(0, (seg1 - seg0 - g + 1) >> 1);  // tiles seg0 + g, seg0 + g + 2, ...
-    auto position = [&](int i) { return i < n_mine ? G.position((seg0 + g + 2 * i) * kTile + key) : -1; };
-    auto fetch = [&](int i, int pos, int pg) {
-      const auto place = [](int row, int piece) { return row * kKv4Row + ((piece ^ ((row >> 1) & 3)) << 4); };
-      G.fetch(ring_at + (i % kTcRing) * kStageBytes, pos, pg, lane, &S.bad[turn], place, place);
-    };
-    int pos_next, pg_next, pos_then;  // of this group's tile i + 3, of the one behind it
-    {
-      int pos[kTcRing + 2], pg[kTcRing + 1];
+    n_list = G.n_list;
+    n_tiles = (G.n_all + kTile - 1) / kTile;
+    seg0 = at - u_start;
+    seg1 = min(n_tiles, part.last - u_start);
+    n_mine = max(0, (seg1 - seg0 - g + 1) >> 1);  // tiles seg0 + g, seg0 + g + 2, ...
+    int pos[kTcRing + 2], pg[kTcRing + 1];
 #pragma unroll
-      for (int s = 0; s < kTcRing + 2; ++s) pos[s] = position(s);
+    for (int s = 0; s < kTcRing + 2; ++s) pos[s] = position(G, s);
 #pragma unroll
-      for (int s = 0; s < kTcRing + 1; ++s) pg[s] = G.page(pos[s]);
-#pragma unroll
-      for (int s = 0; s < kTcRing; ++s) {
-        if (s < n_mine) fetch(s, pos[s], pg[s]);
-        cp_commit();
-      }
-      pos_next = pos[kTcRing];
-      pg_next = pg[kTcRing];
-      pos_then = pos[kTcRing + 1];
-    }
+    for (int s = 0; s < kTcRing + 1; ++s) pg[s] = G.page(pos[s]);
+    par0 = par1 = par2 = make_uint2(0u, 0u);
+    if (0 < n_mine) par0 = fetch(G, 0, pos[0], pg[0]);
+    cp_commit();
+    if (1 < n_mine) par1 = fetch(G, 1, pos[1], pg[1]);
+    cp_commit();
+    if (2 < n_mine) par2 = fetch(G, 2, pos[2], pg[2]);
+    cp_commit();
+    pos_next = pos[3];
+    pg_next = pg[3];
+    pos_then = pos[4];
+  };
+  if (part.first < part.last) begin(part.first);
 
+  for (int at = part.first; at < part.last;) {
     // ---- queries ----
-    if (tid == 0) S.qmax = 0;
-    __syncthreads();
-    if (tid == 0) S.bad[turn ^ 1] = 0;
-    look_at_queries<kTcWarps, R>(P, b, h, 0, P.rows, &S.qmax, S.qsum, S.limit);
-    __syncthreads();
-    const int qexp = query_exponent(S.qmax);
-    const float q_up = __int_as_float((127 + qexp) << 23);
-    for (int i = tid; i < N * 16; i += kTcWarps * 32) {
-      const int r = i >> 4, c = i & 15;
-      uint4 x = make_uint4(0u, 0u, 0u, 0u);
-      if (r < P.rows) x = query_word(P, query_at(P, b, h, r) + c * 8, q_up);
-      sts128(q_at + swizzled(r, c, 64), x.x, x.y, x.z, x.w);
+    {
+      Queries<kTcWarps, R> queries;
+      queries.load(P, b, h, 0, P.rows);
+      queries.look(P, 0, P.rows, &S.qmax[turn], S.qsum, S.limit);
+      __syncthreads();
+      const int qexp = query_exponent(S.qmax[turn]);
+      queries.place(P, __int_as_float((127 + qexp) << 23),
+                    [&](int r, int word, int part8, uint2 x) { sts64(q_at + swizzled(r, word, N) + part8 * 8, x.x, x.y); });
+      if (tid < 2 * R) S.base[tid / R][tid % R] = make_float2(S.qsum[tid % R], 0.f);
+      if (tid == 0) S.bad[turn ^ 1] = S.qmax[turn ^ 1] = 0;
+      fence_proxy_async();
+      __syncthreads();
     }
-    if (tid < 2 * R) S.base[tid / R][tid % R] = make_float2(S.qsum[tid % R], 0.f);
-    fence_proxy_async();
-    __syncthreads();
-    const float k_mul = P.scale * 16777216.f * __int_as_float((127 - qexp) << 23);
-    float l[R], z[R], up = 3e38f;  // sum of p, sum of p (y + 8 t) of this thread's positions; w = p t up
+    const float k_mul = P.scale * 16777216.f * __int_as_float((127 - query_exponent(S.qmax[turn])) << 23);
+    const Gather G(P, b, h);
+    float l[CR], z[CR], up = 3e38f;  // sum of p, sum of p (y + 8 t) of this thread's positions; w = p t up
 #pragma unroll
-    for (int r = 0; r < R; ++r) l[r] = z[r] = 0.f;
+    for (int r = 0; r < CR; ++r) l[r] = z[r] = 0.f;
 
-    // K codes of a stage into tensor memory: two to a column, as the masks leave them
+    // half of the K codes of a stage's rows into tensor memory: two to a column, as the masks leave them
     auto k_codes = [&](int i) {
-      const uint32_t row = ring_at + (i % kTcRing) * kStageBytes + lane * kKv4Row;
+      const uint32_t row = ring_at + (i % kTcRing) * kTcStage + lane * 32;
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const uint4 x = lds128(row + ((c ^ piece_of) << 4));
+      for (int c = 0; c < 2; ++c) {
+        const uint4 x = lds128(row + ((c << 4) ^ swap));
         const uint32_t w[4] = {x.x, x.y, x.z, x.w};
         uint32_t a[16];
 #pragma unroll
@@ -221,7 +247,7 @@ __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& par
           a[4 * j] = w[j] & 0x000f000fu, a[4 * j + 1] = w[j] & 0x00f000f0u;
           a[4 * j + 2] = v & 0x000f000fu, a[4 * j + 3] = v & 0x00f000f0u;
         }
-        tm_st16(tm_a + mine + 16 * c, a);
+        tm_st16(tm_a + mine + half * 32 + 16 * c, a);
       }
       tm_wait_st();
     };
@@ -229,7 +255,7 @@ __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& par
       tm_after();
 #pragma unroll
       for (int kk = 0; kk < 8; ++kk)
-        mma_tmem(tm_s, tm_a + kk * 8, operand(q_at + (kk >> 2) * (64 * 128) + (kk & 3) * 32, 16, 1024), shape_word(N, 0), kk > 0);
+        mma_tmem(tm_s, tm_a + kk * 8, operand(q_at + (kk >> 2) * (N * 128) + (kk & 3) * 32, 16, 1024), shape_word(N, 0), kk > 0);
       if (!lost) mma_done(&S.s_bar[g]);
     };
     if (n_mine > 0) {
@@ -237,7 +263,7 @@ __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& par
       __syncwarp();
       k_codes(0);
       tm_before();
-      named_bar_sync(1 + g, 128);
+      named_bar_sync(1 + g, 256);
       // (test hook: the first scores of CTA 0 are never reported, so the bounded waits run out)
       if (elected) start_scores(P.test_lose && blockIdx.x == 0 && at == part.first);
       __syncwarp();
@@ -245,28 +271,29 @@ __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& par
 
 #pragma unroll 1
     for (int i = 0; i < n_mine; ++i) {
-      const uint32_t stage = ring_at + (i % kTcRing) * kStageBytes;
+      const uint32_t stage = ring_at + (i % kTcRing) * kTcStage;
       const bool more = i + 1 < n_mine;
-      const uint2 par = lds64(stage + 2 * kChunk * kKv4Row + lane * 8);
-      const float2 kp = widen16(par.x, P.half), vp = widen16(par.y, P.half);
-      float x[R];
+      const float2 kp = widen16(par0.x, P.half), vp = widen16(par0.y, P.half);
+      par0 = par1;
+      par1 = par2;
+      float x[CR];
       wait_for(&S.s_bar[g], s_turn++);
       tm_after();
 #pragma unroll
-      for (int c = 0; c < R8; ++c) tm_ld8(x + 8 * c, tm_s + mine + 8 * c);
+      for (int c = 0; c < CR; c += 4) tm_ld4(x + c, tm_s + mine + col0 + c);
       if (more) {
         cp_wait<kTcRing - 2>();
         __syncwarp();
         k_codes(i + 1);
       }
 #pragma unroll
-      for (int c = 0; c < R8; ++c) tm_wait_ld8(x + 8 * c);
+      for (int c = 0; c < CR; c += 4) tm_wait_ld4(x + c);
       // scores from the running maximum on
       const float ks = kp.x * k_mul;
       float t = vp.x, y8 = fmaf(8.f, vp.x, vp.y), top = -INFINITY;
-      const float4* base = reinterpret_cast<const float4*>(S.base[g]);
+      const float4* base = reinterpret_cast<const float4*>(S.base[g] + col0);
 #pragma unroll
-      for (int r = 0; r < R; r += 2) {
+      for (int r = 0; r < CR; r += 2) {
         const float4 qm = base[r >> 1];
         x[r] = fmaf(x[r], ks, fmaf(kp.y, qm.x, qm.y));
         x[r + 1] = fmaf(x[r + 1], ks, fmaf(kp.y, qm.z, qm.w));
@@ -280,29 +307,29 @@ __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& par
         if (spoilt) t = y8 = 0.f;
         top = -INFINITY;
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
+        for (int r = 0; r < CR; ++r) {
           if (spoilt) x[r] = NAN;
-          if (pos >= n_list + S.limit[r]) x[r] = -INFINITY;
+          if (pos >= n_list + S.limit[col0 + r]) x[r] = -INFINITY;
           top = fmaxf(top, x[r]);
         }
       }
       // the maximum moves only where a score passes it by 2^8, the weights' scale where one passes 64
       tm_before();
-      const bool raise = named_bar_or(3 + g, 128, top > 8.f || fabsf(t) * up > 64.f || i == 0);
+      const bool raise = named_bar_or(3 + g, 256, top > 8.f || fabsf(t) * up > 64.f || i == 0);
       if (elected && more) start_scores(false);
       __syncwarp();
       if (raise) {
         const auto larger = [](float a, float c) { return fmaxf(a, c); };
 #pragma unroll
-        for (int c = 0; c < R8; ++c) {
-          const float v = of_eight(x + 8 * c, lane, larger);
-          if (lane < 8) S.red[g][wq][8 * c + lane][0] = v;
+        for (int c = 0; c < CR; c += 4) {
+          const float v = of_four(x + c, lane, larger);
+          if (lane < 4) S.red[g][wq][col0 + c + lane][0] = v;
         }
         float t_max = fabsf(t) <= FLT_MAX ? fabsf(t) : 0.f;
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) t_max = fmaxf(t_max, __shfl_xor_sync(0xffffffffu, t_max, o));
         if (lane == 0) S.t_red[g][wq] = t_max;
-        named_bar_sync(1 + g, 128);
+        named_bar_sync(1 + g, 256);
         t_max = fmaxf(fmaxf(S.t_red[g][0], S.t_red[g][1]), fmaxf(S.t_red[g][2], S.t_red[g][3]));
         float up_now = up;
         if (t_max > 0.f) up_now = fminf(up, __int_as_float((127 + min(5 + 127 - (__float_as_int(t_max) >> 23), 100)) << 23));
@@ -313,26 +340,26 @@ __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& par
           tm_after();
         }
 #pragma unroll
-        for (int c = 0; c < R8; ++c) {
-          float o[8];
+        for (int c = 0; c < CR; c += 4) {
+          float o[4];
           if (i > 0) {
-            tm_ld8(o, tm_o + mine + 8 * c);
-            tm_wait_ld8(o);
+            tm_ld4(o, tm_o + mine + col0 + c);
+            tm_wait_ld4(o);
           }
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const int r = 8 * c + e;
+          for (int e = 0; e < 4; ++e) {
+            const int r = col0 + c + e;
             const float v = fmaxf(fmaxf(S.red[g][0][r][0], S.red[g][1][r][0]), fmaxf(S.red[g][2][r][0], S.red[g][3][r][0]));
             // (a query that sees nothing of the group's first tile sees nothing of the later ones)
             const float d = i == 0 ? (v == -INFINITY ? 0.f : v) : fmaxf(v, 0.f);
             const float f = ex2(-d);
-            x[r] -= d;
-            l[r] *= f;
-            z[r] *= f;
+            x[c + e] -= d;
+            l[c + e] *= f;
+            z[c + e] *= f;
             o[e] *= f * scale_now;
-            if ((tid & 127) == r) S.base[g][r].y -= d;
+            if (key == r) S.base[g][r].y -= d;
           }
-          if (i > 0) tm_st8(tm_o + mine + 8 * c, o);
+          if (i > 0) tm_st4(tm_o + mine + col0 + c, o);
         }
         tm_wait_st();
       }
@@ -342,43 +369,42 @@ __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& par
         tm_after();
       }
       {
-        const uint32_t row = stage + (kChunk + lane) * kKv4Row;
+        const uint32_t row = stage + (kChunk + lane) * 32;
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          const uint4 raw = lds128(row + ((c ^ piece_of) << 4));
+        for (int c = 0; c < 2; ++c) {
+          const uint4 raw = lds128(row + ((c << 4) ^ swap));
           const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             const uint32_t v = w[j] >> 8;
-            sts128(v_at + swizzled(key, 4 * c + j, kTile), minus(w[j] & 0x000f000fu, 0x00080008u), minus(w[j] & 0x00f000f0u, 0x00800080u),
-                   minus(v & 0x000f000fu, 0x00080008u), minus(v & 0x00f000f0u, 0x00800080u));
+            sts128(v_at + swizzled(key, 8 * half + 4 * c + j, kTile), minus(w[j] & 0x000f000fu, 0x00080008u),
+                   minus(w[j] & 0x00f000f0u, 0x00800080u), minus(v & 0x000f000fu, 0x00080008u), minus(v & 0x00f000f0u, 0x00800080u));
           }
         }
       }
       __syncwarp();  // the stage has been read
-      if (i + kTcRing < n_mine) fetch(i + kTcRing, pos_next, pg_next);
+      if (i + kTcRing < n_mine) par2 = fetch(G, i + kTcRing, pos_next, pg_next);
       cp_commit();
       pos_next = pos_then;
       pg_next = G.page(pos_then);
-      pos_then = position(i + kTcRing + 2);
+      pos_then = position(G, i + kTcRing + 2);
       // weights
       const float w_of = t * up;
 #pragma unroll
-      for (int c = 0; c < R8; ++c) {
-        uint32_t w[4];
+      for (int c = 0; c < CR; c += 4) {
+        float p[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const int r = 8 * c + 2 * e;
-          const float p0 = ex2(x[r]), p1 = ex2(x[r + 1]);
-          l[r] += p0, l[r + 1] += p1;
-          z[r] = fmaf(p0, y8, z[r]), z[r + 1] = fmaf(p1, y8, z[r + 1]);
-          w[e] = pack_f16(p0 * w_of, p1 * w_of);
+          p[e] = ex2(x[c + e]);
+          l[c + e] += p[e];
+          z[c + e] = fmaf(p[e], y8, z[c + e]);
         }
-        sts128(w_at + key * 128 + ((c ^ (key & 7)) << 4), w[0], w[1], w[2], w[3]);
+        const int r = col0 + c;
+        sts64(w_at + key * 128 + (((r >> 3) ^ (key & 7)) << 4) + (r & 4) * 2, pack_f16(p[0] * w_of, p[1] * w_of), pack_f16(p[2] * w_of, p[3] * w_of));
       }
       fence_proxy_async();
       tm_before();
-      named_bar_sync(1 + g, 128);
+      named_bar_sync(1 + g, 256);
       if (elected) {
         tm_after();
 #pragma unroll
@@ -389,61 +415,10 @@ __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& par
       __syncwarp();
     }
     cp_wait<0>();
-    if (n_mine > 0) {
-      wait_for(&S.o_bar[g], o_turn++);
-      tm_after();
-    }
 
     // ---- the groups' parts meet ----
-    const auto add = [](float a, float c) { return a + c; };
-#pragma unroll
-    for (int c = 0; c < R8; ++c) {
-      const float ls = of_eight(l + 8 * c, lane, add), zs = of_eight(z + 8 * c, lane, add);
-      if (lane < 8) S.red[g][wq][8 * c + lane][0] = ls, S.red[g][wq][8 * c + lane][1] = zs;
-    }
-    __syncthreads();  // both groups are done with their operands: records take their place
-    float* meet = reinterpret_cast<float*>(smem);
-    static_assert(R8 % 2 == 0 || 2 * R * kRowFloats * 4 <= 65536, "the spare columns of W have to stay zero");
-    if ((tid & 127) < R) {
-      const int r = tid & 127;
-      const float ls = (S.red[g][0][r][0] + S.red[g][1][r][0]) + (S.red[g][2][r][0] + S.red[g][3][r][0]);
-      S.sums[g][r][1] = (S.red[g][0][r][1] + S.red[g][1][r][1]) + (S.red[g][2][r][1] + S.red[g][3][r][1]);
-      float* rec = meet + (g * R + r) * kRowFloats;
-      rec[kKv4D] = ls == 0.f ? -FLT_MAX : -S.base[g][r].y;
-      rec[kKv4D + 1] = ls;
-    }
-    named_bar_sync(1 + g, 128);
-    {
-      // lane 8 i + j of O^T is element 8 i + (0, 4, 1, 5, 2, 6, 3, 7)[j], of the high half of a byte where j has bit 1
-      const int j = key & 7, d = (key & ~7) + ((j & 1) << 2) + (j >> 1);
-      const float down = (j & 2 ? 1048576.f : 16777216.f) / up;
-#pragma unroll
-      for (int c = 0; c < R8; ++c) {
-        float o[8];
-        if (n_mine > 0) {
-          tm_ld8(o, tm_o + mine + 8 * c);
-          tm_wait_ld8(o);
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          meet[(g * R + 8 * c + e) * kRowFloats + d] = n_mine > 0 ? fmaf(o[e], down, S.sums[g][8 * c + e][1]) : 0.f;
-      }
-    }
-    tm_before();
-    __syncthreads();
-    tm_after();
-    const bool whole = seg0 == 0 && seg1 == n_tiles;
-    float* rec = P.partial + static_cast<long long>(2 * blockIdx.x + (seg0 == 0 ? 1 : 0)) * units.rows * kRowFloats;
-    finish<kTcWarps, 2, R>(P, meet, b, h, 0, P.rows, whole, rec);
-    if (tid == 0) {
-      const int flag = S.bad[turn] | (S.abort ? SPECATTN_ROW_TIMEOUT : 0);
-      if (whole)
-        P.flags[u] = flag;
-      else
-        rec[kKv4D + 2] = __int_as_float(flag);
-    }
-    turn ^= 1;
-    __syncthreads();  // the records have been read
+    const int this_u = u, this_b = b, this_h = h, this_mine = n_mine, this_turn = turn;
+    const bool first_part = seg0 == 0, whole = seg0 == 0 && seg1 == n_tiles;
     at = u_start + seg1;
     if (seg1 == n_tiles) {
       u_start += n_tiles;
@@ -451,6 +426,61 @@ __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& par
         ++u;
       } while (u < units.n && at < part.last && chunks_of(P, u, kTile) == 0);
     }
+    turn ^= 1;
+    if (at < part.last) begin(at);
+    if (this_mine > 0) {
+      wait_for(&S.o_bar[g], o_turn++);
+      tm_after();
+    }
+    const auto add = [](float a, float c) { return a + c; };
+#pragma unroll
+    for (int c = 0; c < CR; c += 4) {
+      const float ls = of_four(l + c, lane, add), zs = of_four(z + c, lane, add);
+      if (lane < 4) S.red[g][wq][col0 + c + lane][0] = ls, S.red[g][wq][col0 + c + lane][1] = zs;
+    }
+    __syncthreads();  // both groups are done with their operands: records take their place
+    float* meet = reinterpret_cast<float*>(smem);
+    static_assert(R8 % 2 == 0 || 2 * R * kRowFloats * 4 <= 65536, "the spare columns of W have to stay zero");
+    if ((tid & 255) < R) {
+      const int r = tid & 255;
+      const float ls = (S.red[g][0][r][0] + S.red[g][1][r][0]) + (S.red[g][2][r][0] + S.red[g][3][r][0]);
+      S.sums[g][r] = (S.red[g][0][r][1] + S.red[g][1][r][1]) + (S.red[g][2][r][1] + S.red[g][3][r][1]);
+      float* rec = meet + (g * R + r) * kRowFloats;
+      rec[kKv4D] = ls == 0.f ? -FLT_MAX : -S.base[g][r].y;
+      rec[kKv4D + 1] = ls;
+    }
+    named_bar_sync(1 + g, 256);
+    {
+      // lane 8 i + j of O^T is element 8 i + (0, 4, 1, 5, 2, 6, 3, 7)[j], of the high half of a byte where j has bit 1
+      const int j = key & 7, d = (key & ~7) + ((j & 1) << 2) + (j >> 1);
+      const float down = (j & 2 ? 1048576.f : 16777216.f) / up;
+#pragma unroll
+      for (int c = 0; c < CR; c += 4) {
+        float o[4];
+        if (this_mine > 0) {
+          tm_ld4(o, tm_o + mine + col0 + c);
+          tm_wait_ld4(o);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int r = col0 + c + e;
+          meet[(g * R + r) * kRowFloats + d] = this_mine > 0 ? fmaf(o[e], down, S.sums[g][r]) : 0.f;
+        }
+      }
+    }
+    tm_before();
+    __syncthreads();
+    tm_after();
+    float* rec = P.partial + static_cast<long long>(2 * blockIdx.x + (first_part ? 1 : 0)) * units.rows * kRowFloats;
+    finish<kTcWarps, 2, R>(P, meet, this_b, this_h, 0, P.rows, whole, rec);
+    if (tid == 0) {
+      const int flag = S.bad[this_turn] | (S.abort ? SPECATTN_ROW_TIMEOUT : 0);
+      if (whole)
+        P.flags[this_u] = flag;
+      else
+        rec[kKv4D + 2] = __int_as_float(flag);
+    }
+    __syncthreads();  // the records have been read
   }
   __syncthreads();
   if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(S.tmem), "r"(512u) : "memory");

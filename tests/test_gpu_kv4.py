@@ -167,8 +167,7 @@ ENGINES = {"auto": 0, "mma.sync": 2, "tcgen05": 4}
 
 
 def _engines(T, Hq, Hkv):
-    """What may run that many query rows."""
-    return ["mma.sync", "tcgen05"] if T * (Hq // Hkv) > 16 else ["auto"]
+    return ["mma.sync", "tcgen05"]
 
 
 def _run(c, engine="auto", **kw):
