@@ -255,10 +255,25 @@ extern "C" int specattn_kv4_verify(const specattn_kv4_verify_args* args, void* c
   const int sms = device_sm_count();
   if (sms <= 0) return SPECATTN_ERR_CUDA;
   if (A.workspace_bytes < workspace_bytes(A, sms)) return SPECATTN_ERR_WORKSPACE;
+  const specattn_kv4_cache& cache = A.cache;
+  // the kernel addresses codes in 16-byte and params in 4-byte units of 32 bits
+  const double reach = (static_cast<double>(cache.n_pages) * cache.stride_page + cache.stride_kv +
+                        static_cast<double>(cache.page_size) * cache.stride_slot) / 16;
+  const double reach_params = (static_cast<double>(cache.n_pages) * cache.pstride_page + cache.pstride_kv +
+                               static_cast<double>(cache.page_size) * cache.pstride_slot) / 2;
+  if (cache.stride_page < 0 || cache.stride_kv < 0 || cache.stride_slot < 0 || cache.stride_head < 0 || cache.pstride_page < 0 ||
+      cache.pstride_kv < 0 || cache.pstride_slot < 0 || cache.pstride_head < 0 || reach >= 4294967296. || reach_params >= 4294967296. ||
+      cache.block_table_stride > INT32_MAX)
+    return SPECATTN_ERR_UNSUPPORTED;
   const int r8 = query_tiles(A), groups = groups_of(r8);
   Kv4Params P;
   memset(&P, 0, sizeof(P));
   P.cache = kv4_view(A.cache);
+  P.c_page = static_cast<unsigned>(cache.stride_page / 16);
+  P.c_slot = static_cast<unsigned>(cache.stride_slot / 16);
+  P.p_page = static_cast<unsigned>(cache.pstride_page / 2);
+  P.p_slot = static_cast<unsigned>(cache.pstride_slot / 2);
+  P.pages_per_seq = static_cast<int>(cache.block_table_stride);
   P.q = static_cast<const unsigned char*>(A.q);
   P.kv_len = A.kv_len;
   P.idx = A.idx;

@@ -34,6 +34,8 @@ struct Kv4Params {
   int B, T, Hq, H, grp, rows, G, dense, tail, out_f32, half;
   int groups_of_rows, rows_per_group;  // of the mma.sync path
   int most_units;                      // of either path
+  unsigned c_page, c_slot, p_page, p_slot;  // strides of codes in 16-byte, of params in 4-byte units
+  int pages_per_seq;
   int engine, test_lose;               // 1: mma.sync, 2: tcgen05, 0: by the lengths
 };
 
@@ -48,6 +50,35 @@ __device__ __forceinline__ Units units_of(const Kv4Params& P, int tensor) {
   return u;
 }
 
+// Two binary32 operations in one instruction.
+struct Two {
+  unsigned long long v;
+};
+__device__ __forceinline__ Two two(float a, float b) {
+  Two r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float2 each(Two a) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(a.v));
+  return r;
+}
+__device__ __forceinline__ Two fma2(Two a, Two b, Two c) {
+  Two r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return r;
+}
+__device__ __forceinline__ Two mul2(Two a, Two b) {
+  Two r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ Two add2(Two a, Two b) {
+  Two r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   const __half2 v = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&v);
@@ -187,47 +218,49 @@ __device__ __forceinline__ Partition cut(const Kv4Params& P, int tensor, int chu
   return p;
 }
 
-// The positions of one unit, looked up and fetched by warps.
+// The positions of one unit, looked up and fetched by warps.  Rows are addressed in 16-byte (codes) and 4-byte
+// (params) units of 32 bits, which reach 64 GB of codes: a lookup is a dozen instructions instead of fifty.
 struct Gather {
   const Kv4Params& P;
-  int b, h, n_list, n_all, ctx;
-  const int* list;
+  int n_list, n_all, ctx;
+  const int *list, *table;
+  const unsigned char *codes, *params;  // of this head
+  int first_page;                       // without a table
 
-  __device__ __forceinline__ Gather(const Kv4Params& p, int b_, int h_) : P(p), b(b_), h(h_) {
+  __device__ __forceinline__ Gather(const Kv4Params& p, int b, int h) : P(p) {
     n_list = list_len(P, b, h);
     n_all = n_list + P.tail;
     ctx = max(0, P.kv_len[b]);
     list = P.dense ? nullptr : P.idx + (static_cast<long long>(b) * P.G + (P.G > 1 ? h : 0)) * P.idx_stride;
+    table = P.cache.table != nullptr ? P.cache.table + b * P.cache.table_stride : nullptr;
+    first_page = static_cast<int>(min(b * P.cache.table_stride, P.cache.n_pages));  // (n_pages fits; beyond it no page is)
+    codes = P.cache.codes + h * P.cache.s_head;
+    params = P.cache.params + h * P.cache.p_head;
   }
-  __device__ __forceinline__ int position(int i) const {  // the i-th position; -1: none, -2: out of range
-    if (i >= n_all) return -1;
-    if (i >= n_list) return ctx + (i - n_list);
-    const int pos = P.dense ? i : list[i];
-    return pos >= 0 && pos < ctx ? pos : -2;
+  // The three steps to the i-th row, made a tile or more apart: what a step loads is looked at by the next one only, since a
+  // warp that compared it at once would wait for it (900 cycles a tile).
+  __device__ __forceinline__ int position(int i) const {
+    if (i >= n_all) return 0;
+    return i >= n_list ? ctx + (i - n_list) : P.dense ? i : list[i];
   }
-  __device__ __forceinline__ int page(int pos) const {
-    if (pos == -1) return -1;
-    if (pos >= 0) {
-      const long long p = page_of(P.cache.table, P.cache.table_stride, P.cache.n_pages, b, pos / P.cache.by_page);
-      if (p >= 0) return static_cast<int>(p);
-    }
-    return -2;
+  __device__ __forceinline__ int page(int i, int pos) const {  // -2: none
+    const int pi = pos / P.cache.by_page;  // (of a negative position: anything)
+    if (i >= n_all || pos < 0 || (i < n_list && pos >= ctx) || pi >= P.pages_per_seq) return -2;
+    return table != nullptr ? table[pi] : static_cast<int>(static_cast<unsigned>(first_page) + pi);
   }
-  // Where a row lies: bytes from the codes' and the params' beginning; position 0 / page 0 where a position or page is
-  // out of range.
-  __device__ __forceinline__ long long locate(int pos, int pg, int* bad, long long* params) const {
-    *params = 0;
-    if (pos == -1) return 0;
-    int slot = 0;
-    if (pg < 0) {
+  // Where the row lies: units from `codes` and `params`.  Position 0 / page 0 where position or page is out of range.
+  __device__ __forceinline__ uint2 locate(int i, int pos, int pg, int* bad) const {
+    if (i >= n_all) return make_uint2(0u, 0u);
+    unsigned slot = static_cast<unsigned>(pos - pos / P.cache.by_page * P.cache.page_size);
+    if (static_cast<unsigned>(pg) >= static_cast<unsigned>(P.cache.n_pages)) {
       *bad = SPECATTN_ROW_BAD_INDEX;
       pg = 0;
-    } else {
-      slot = pos - pos / P.cache.by_page * P.cache.page_size;
+      slot = 0;
     }
-    *params = pg * P.cache.p_page + slot * P.cache.p_slot + h * P.cache.p_head;
-    return pg * P.cache.s_page + slot * P.cache.s_slot + h * P.cache.s_head;
+    return make_uint2(pg * P.c_page + slot * P.c_slot, pg * P.p_page + slot * P.p_slot);
   }
+  __device__ __forceinline__ const unsigned char* code_row(uint32_t at) const { return codes + static_cast<unsigned long long>(at) * 16; }
+  __device__ __forceinline__ const unsigned char* param_row(uint32_t at) const { return params + static_cast<unsigned long long>(at) * 4; }
 };
 
 // A query row's first element.

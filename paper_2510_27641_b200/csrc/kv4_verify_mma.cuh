@@ -67,21 +67,22 @@ __device__ __forceinline__ void mma_path(const Kv4Params& P, const Partition& pa
     const int seg0 = at - u_start, seg1 = min(n_chunks, part.last - u_start);  // chunks of the unit
     const int row0 = rg * units.rows, n_rows = min(units.rows, P.rows - row0);
 
-    auto position = [&](int chunk) { return chunk < seg1 ? G.position(chunk * kChunk + lane) : -1; };
+    auto position = [&](int chunk) { return chunk < seg1 ? G.position(chunk * kChunk + lane) : 0; };
+    auto page = [&](int chunk, int pos) { return chunk < seg1 ? G.page(chunk * kChunk + lane, pos) : -2; };
     // The warp copies its 32 rows to a stage: K rows, V rows, then (s, z, t, y) of each.
     auto fetch = [&](int chunk, int pos, int pg) {
       const uint32_t stage = ring_at + ((chunk / NWARP) % STAGES) * kStageBytes;
-      long long par;
-      const long long off = G.locate(pos, pg, &S.bad[turn], &par);
-      const int bytes = pos != -1 ? 4 : 0;  // (a position that is none leaves zeros for scale and zero point, and any codes)
-      cp_async4(stage + 2 * kChunk * kKv4Row + lane * 8, P.cache.params + par, bytes);
-      cp_async4(stage + 2 * kChunk * kKv4Row + lane * 8 + 4, P.cache.params + par + P.cache.p_kv, bytes);
+      const uint2 row_at = G.locate(chunk * kChunk + lane, pos, pg, &S.bad[turn]);
+      const unsigned char* par = G.param_row(row_at.y);
+      const int bytes = chunk * kChunk + lane < G.n_all ? 4 : 0;  // (a position that is none leaves zeros for scale and zero point, and any codes)
+      cp_async4(stage + 2 * kChunk * kKv4Row + lane * 8, par, bytes);
+      cp_async4(stage + 2 * kChunk * kKv4Row + lane * 8 + 4, par + P.cache.p_kv, bytes);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         // four lanes a row.  K rows lie in order.  Row j of a V tile of 16 lies where the second product's lanes find
         // it without bank conflicts: 2 t -> t, 2 t + 1 -> t + 4 within eight, its 32-byte halves swapped by bit 1.
         const int row = j * 8 + g, r8 = row & 7, v_row = (row & ~7) | ((r8 >> 1) | ((r8 & 1) << 2));
-        const unsigned char* from = P.cache.codes + __shfl_sync(0xffffffffu, off, row) + t * 16;
+        const unsigned char* from = G.code_row(__shfl_sync(0xffffffffu, row_at.x, row) + t);
         cp_async16(stage + row * kKv4Row + t * 16, from);
         cp_async16(stage + (kChunk + v_row) * kKv4Row + ((t * 16) ^ ((v_row & 2) << 4)), from + P.cache.s_kv);
       }
@@ -97,7 +98,7 @@ __device__ __forceinline__ void mma_path(const Kv4Params& P, const Partition& pa
 #pragma unroll
       for (int s = 0; s <= STAGES; ++s) pos[s] = position(first + s * NWARP);
 #pragma unroll
-      for (int s = 0; s < STAGES; ++s) pg[s] = G.page(pos[s]);
+      for (int s = 0; s < STAGES; ++s) pg[s] = page(first + s * NWARP, pos[s]);
 #pragma unroll
       for (int s = 0; s < STAGES - 1; ++s) {
         if (first + s * NWARP < seg1) fetch(first + s * NWARP, pos[s], pg[s]);
@@ -120,7 +121,7 @@ __device__ __forceinline__ void mma_path(const Kv4Params& P, const Partition& pa
     });
     sync();
     const float k_mul = P.scale * 16777216.f * __int_as_float((127 - qexp) << 23);  // codes are c 2^-24 in the product
-    float sq[NT][2], m[NT][2], l[NT][2], y[NT][2];  // sum q; running maximum (log2), sum of p, sum of p (y + 8 t)
+    Two sq[NT], m[NT], l[NT], y[NT];  // of two queries: sum q; minus the running maximum (log2), sum of p, sum of p (y + 8 t)
     float acc[8][NT][4], acc8[NT][4];                // output by (element tile, query tile), less its middle
     float up = 3e38f;                                // the weights' power of two: w = p t up
 #pragma unroll
@@ -131,8 +132,8 @@ __device__ __forceinline__ void mma_path(const Kv4Params& P, const Partition& pa
 #pragma unroll
         for (int mt = 0; mt < 8; ++mt) acc[mt][nt][e] = 0.f;
       }
-#pragma unroll
-      for (int e = 0; e < 2; ++e) sq[nt][e] = S.qsum[nt * 8 + 2 * t + e], m[nt][e] = 0.f, l[nt][e] = 0.f, y[nt][e] = 0.f;
+      sq[nt] = two(S.qsum[nt * 8 + 2 * t], S.qsum[nt * 8 + 2 * t + 1]);
+      m[nt] = l[nt] = y[nt] = two(0.f, 0.f);
     }
     const uint2* q_op = reinterpret_cast<const uint2*>(smem) + lane;
 
@@ -145,7 +146,7 @@ __device__ __forceinline__ void mma_path(const Kv4Params& P, const Partition& pa
         if (ahead < seg1) fetch(ahead, pos_next, pg_next);
         cp_commit();
         pos_next = pos_then;
-        pg_next = G.page(pos_then);
+        pg_next = page(ahead + NWARP, pos_then);
         pos_then = position(ahead + 2 * NWARP);
       }
       const uint32_t stage = ring_at + ((chunk / NWARP) % STAGES) * kStageBytes;
@@ -200,9 +201,10 @@ __device__ __forceinline__ void mma_path(const Kv4Params& P, const Partition& pa
           y_of[h2][r] = fmaf(8.f, vp.x, vp.y);
           t_max = fmaxf(t_max, fabsf(vp.x));
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) s[h2][nt][2 * r + e] = fmaf(s[h2][nt][2 * r + e], ks, fmaf(kp.y, sq[nt][e], -m[nt][e]));
+          for (int nt = 0; nt < NT; ++nt) {
+            const float2 x2 = each(fma2(two(s[h2][nt][2 * r], s[h2][nt][2 * r + 1]), two(ks, ks), fma2(two(kp.y, kp.y), sq[nt], m[nt])));
+            s[h2][nt][2 * r] = x2.x, s[h2][nt][2 * r + 1] = x2.y;
+          }
         }
       // what a query does not see: past the end, or behind it in the tail.  (A masked row may hold anything, and 0 NaN is
       // NaN: what a tail row's V scale would spoil, its scores spoil instead.)
@@ -243,7 +245,7 @@ __device__ __forceinline__ void mma_path(const Kv4Params& P, const Partition& pa
         up = up_now;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-          float f[2];
+          float f[2], down[2];
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             float v = fmaxf(fmaxf(s[0][nt][e], s[0][nt][2 + e]), fmaxf(s[1][nt][e], s[1][nt][2 + e]));
@@ -253,12 +255,14 @@ __device__ __forceinline__ void mma_path(const Kv4Params& P, const Partition& pa
             // (a query that sees nothing of the warp's first chunk sees nothing of the later ones)
             const float d = chunk == first ? (v == -INFINITY ? 0.f : v) : fmaxf(v, 0.f);
             f[e] = ex2(-d);
-            m[nt][e] += d;
-            l[nt][e] *= f[e];
-            y[nt][e] *= f[e];
-            f[e] = chunk == first ? 0.f : f[e] * scale_now;
+            down[e] = d;
             s[0][nt][e] -= d, s[0][nt][2 + e] -= d, s[1][nt][e] -= d, s[1][nt][2 + e] -= d;
           }
+          m[nt] = add2(m[nt], two(-down[0], -down[1]));
+          l[nt] = mul2(l[nt], two(f[0], f[1]));
+          y[nt] = mul2(y[nt], two(f[0], f[1]));
+#pragma unroll
+          for (int e = 0; e < 2; ++e) f[e] = chunk == first ? 0.f : f[e] * scale_now;
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             acc8[nt][e] *= f[e & 1];
@@ -277,10 +281,11 @@ __device__ __forceinline__ void mma_path(const Kv4Params& P, const Partition& pa
           const float w_of = h2 ? -t_of[h2][r] * up : t_of[h2][r] * up;
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
-            const float p0 = ex2(s[h2][nt][2 * r]), p1 = ex2(s[h2][nt][2 * r + 1]);
-            l[nt][0] += p0, l[nt][1] += p1;
-            y[nt][0] = fmaf(p0, y_of[h2][r], y[nt][0]), y[nt][1] = fmaf(p1, y_of[h2][r], y[nt][1]);
-            pb[nt][r] = transpose8(pack_f16(p0 * w_of, p1 * w_of));
+            const Two p = two(ex2(s[h2][nt][2 * r]), ex2(s[h2][nt][2 * r + 1]));
+            l[nt] = add2(l[nt], p);
+            y[nt] = fma2(p, two(y_of[h2][r], y_of[h2][r]), y[nt]);
+            const float2 w = each(mul2(p, two(w_of, w_of)));
+            pb[nt][r] = transpose8(pack_f16(w.x, w.y));
           }
         }
         // V rows of positions 2 t, 2 t + 1, 2 t + 8, 2 t + 9 of the tile, 8 bytes to a lane
@@ -325,14 +330,14 @@ __device__ __forceinline__ void mma_path(const Kv4Params& P, const Partition& pa
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          float ls = l[nt][e], ys = y[nt][e];
+          float ls = e ? each(l[nt]).y : each(l[nt]).x, ys = e ? each(y[nt]).y : each(y[nt]).x;
 #pragma unroll
           for (int o = 4; o < 32; o <<= 1) {
             ls += __shfl_xor_sync(0xffffffffu, ls, o);
             ys += __shfl_xor_sync(0xffffffffu, ys, o);
           }
           float* rec = meet + (warp * K::kQueries + nt * 8 + 2 * t + e) * kRowFloats;
-          if (g == 0) rec[kKv4D] = ls == 0.f ? -FLT_MAX : m[nt][e], rec[kKv4D + 1] = ls;
+          if (g == 0) rec[kKv4D] = ls == 0.f ? -FLT_MAX : -(e ? each(m[nt]).y : each(m[nt]).x), rec[kKv4D + 1] = ls;
           const float mid = acc8[nt][e];
           // lane g has elements 16 g ... 16 g + 15: tile mt holds 2 mt (codes in the low half of a byte) and 2 mt + 1
 #pragma unroll

@@ -32,7 +32,7 @@ constexpr int kTcSmem = 2 * 32768 + 2 * 16384 + 16384 + kTcWarps * kTcRing * kTc
 
 struct Tc4Shared {
   alignas(8) unsigned long long s_bar[2], o_bar[2];
-  alignas(16) float2 base[2][64];  // (sum q, minus the running maximum) of a group's queries
+  alignas(16) float4 base[2][32];  // of two of a group's queries: sums q, minus the running maxima
   float red[2][4][64][2];          // what the warps of a group reduce
   float t_red[2][4];
   float sums[2][64];  // sum of p (y + 8 t)
@@ -56,18 +56,25 @@ __device__ __forceinline__ uint64_t operand(uint32_t at, uint32_t leading, uint3
 __device__ __forceinline__ uint32_t shape_word(int n, uint32_t mn_major) {
   return (1u << 4) | (mn_major << 15) | (mn_major << 16) | (static_cast<uint32_t>(n >> 3) << 17) | (8u << 24);
 }
+// One thread of the warp, chosen by the hardware.  (Behind a branch on a thread's number descriptors go through vector
+// registers: 8 products of 128 x 48 x 16 from tensor memory then take 760 cycles to issue and finish instead of 390.)
+__device__ __forceinline__ bool elect() {
+  uint32_t p;
+  asm volatile("{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(p));
+  return p != 0;
+}
 __device__ __forceinline__ void mma_smem(uint32_t d, uint64_t a, uint64_t b, uint32_t shape, uint32_t acc) {
   asm volatile(
       "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, {%5, %5, %5, %5}, p;\n\t}" ::"r"(d),
-      "l"(a), "l"(b), "r"(shape), "r"(acc), "r"(0u)
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+      "l"(a), "l"(b), "r"(shape), "r"(acc)
       : "memory");
 }
 __device__ __forceinline__ void mma_tmem(uint32_t d, uint32_t a, uint64_t b, uint32_t shape, uint32_t acc) {
   asm volatile(
       "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, {%5, %5, %5, %5}, p;\n\t}" ::"r"(d),
-      "r"(a), "l"(b), "r"(shape), "r"(acc), "r"(0u)
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+      "r"(a), "l"(b), "r"(shape), "r"(acc)
       : "memory");
 }
 __device__ __forceinline__ void mma_done(unsigned long long* bar) {
@@ -78,6 +85,9 @@ __device__ __forceinline__ void tm_after() { asm volatile("tcgen05.fence::after_
 // (the values pass through, so that nothing that uses them moves ahead of the wait)
 __device__ __forceinline__ void tm_wait_ld4(float* r) {
   asm volatile("tcgen05.wait::ld.sync.aligned;" : "+f"(r[0]), "+f"(r[1]), "+f"(r[2]), "+f"(r[3])::"memory");
+}
+__device__ __forceinline__ void tm_pass4(float* r) {  // (for the values of a wait that has been made)
+  asm volatile("" : "+f"(r[0]), "+f"(r[1]), "+f"(r[2]), "+f"(r[3])::"memory");
 }
 __device__ __forceinline__ void tm_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tm_ld4(float* r, uint32_t at) {
@@ -152,7 +162,8 @@ __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& par
   __syncthreads();
   tm_after();
   const uint32_t tm_a = S.tmem + g * 192, tm_s = tm_a + 64, tm_o = tm_a + 128, mine = static_cast<uint32_t>(wq * 32) << 16;
-  const bool elected = (tid & 255) == 0;
+  const uint64_t q_op = operand(q_at, 16, 1024), v_op = operand(v_at, kTile * 128, 1024), w_op = operand(w_at, 16384, 1024);
+  const bool issues = (__shfl_sync(0xffffffffu, warp, 0) & 7) == 0;  // a warp of each group
   uint32_t s_turn = 0, o_turn = 0;  // completions of this group's products that have been waited for
   auto wait_for = [&](unsigned long long* bar, uint32_t turn) {
     if (!mbar_wait(bar, turn & 1u, &S.abort)) S.abort = 1;
@@ -161,26 +172,32 @@ __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& par
 
   int u = part.unit, u_start = part.start, turn = 0;
   int b = 0, h = 0, seg0 = 0, seg1 = 0, n_tiles = 0, n_mine = 0, n_list = 0;
-  int pos_next = -1, pg_next = -1, pos_then = -1;  // of this group's tile i + 3, of the one behind it
-  uint2 par0, par1, par2;                          // (s, z), (t, y) of this thread's position in tiles i, i + 1, i + 2
-  auto position = [&](const Gather& G, int i) { return i < n_mine ? G.position((seg0 + g + 2 * i) * kTile + key) : -1; };
-  // the warp copies its halves of 32 rows to a stage, K then V, two lanes to a row; scales come straight
-  auto fetch = [&](const Gather& G, int i, int pos, int pg) {
+  int pos_next = 0, pg_next = -2, pos_then = 0;  // of this group's tile i + 3, of the one behind it
+  uint32_t par_at1 = ~0u, par_at2 = ~0u;           // where its scales lie: of tiles i + 1, i + 2
+  uint2 par;                                       // (s, z), (t, y) of this thread's position in the next tile
+  auto index = [&](int i) { return (seg0 + g + 2 * i) * kTile + key; };  // in the unit, of this thread's position in the group's tile i
+  auto position = [&](const Gather& G, int i) { return i < n_mine ? G.position(index(i)) : 0; };
+  auto page = [&](const Gather& G, int i, int pos) { return i < n_mine ? G.page(index(i), pos) : -2; };
+  // the warp copies its halves of 32 rows to a stage, K then V, two lanes to a row; the scales' place is returned, ~0: none
+  auto fetch = [&](const Gather& G, int i, int pos, int pg) -> uint32_t {
     const uint32_t stage = ring_at + (i % kTcRing) * kTcStage;
-    long long par;
-    const long long off = G.locate(pos, pg, &S.bad[turn], &par);
-    uint2 x = make_uint2(0u, 0u);
-    if (pos != -1) {
-      x.x = *reinterpret_cast<const uint32_t*>(P.cache.params + par);
-      x.y = *reinterpret_cast<const uint32_t*>(P.cache.params + par + P.cache.p_kv);
-    }
+    const uint2 row_at = G.locate(index(i), pos, pg, &S.bad[turn]);
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       const int row = j * 16 + (lane >> 1);
-      const unsigned char* from = P.cache.codes + __shfl_sync(0xffffffffu, off, row) + half * 32 + (lane & 1) * 16;
+      const unsigned char* from = G.code_row(__shfl_sync(0xffffffffu, row_at.x, row) + half * 2 + (lane & 1));
       const uint32_t to = stage + row * 32 + (((lane & 1) ^ ((row >> 2) & 1)) << 4);
       cp_async16(to, from);
       cp_async16(to + kChunk * 32, from + P.cache.s_kv);
+    }
+    return index(i) < G.n_all ? row_at.y : ~0u;
+  };
+  auto scales = [&](const Gather& G, uint32_t place) {  // (zeros where there is no position)
+    uint2 x = make_uint2(0u, 0u);
+    if (place != ~0u) {
+      const unsigned char* from = G.param_row(place);
+      x.x = *reinterpret_cast<const uint32_t*>(from);
+      x.y = *reinterpret_cast<const uint32_t*>(from + P.cache.p_kv);
     }
     return x;
   };
@@ -198,13 +215,13 @@ __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& par
 #pragma unroll
     for (int s = 0; s < kTcRing + 2; ++s) pos[s] = position(G, s);
 #pragma unroll
-    for (int s = 0; s < kTcRing + 1; ++s) pg[s] = G.page(pos[s]);
-    par0 = par1 = par2 = make_uint2(0u, 0u);
-    if (0 < n_mine) par0 = fetch(G, 0, pos[0], pg[0]);
+    for (int s = 0; s < kTcRing + 1; ++s) pg[s] = page(G, s, pos[s]);
+    par_at1 = par_at2 = ~0u;
+    if (0 < n_mine) par = scales(G, fetch(G, 0, pos[0], pg[0]));
     cp_commit();
-    if (1 < n_mine) par1 = fetch(G, 1, pos[1], pg[1]);
+    if (1 < n_mine) par_at1 = fetch(G, 1, pos[1], pg[1]);
     cp_commit();
-    if (2 < n_mine) par2 = fetch(G, 2, pos[2], pg[2]);
+    if (2 < n_mine) par_at2 = fetch(G, 2, pos[2], pg[2]);
     cp_commit();
     pos_next = pos[3];
     pg_next = pg[3];
@@ -222,16 +239,17 @@ __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& par
       const int qexp = query_exponent(S.qmax[turn]);
       queries.place(P, __int_as_float((127 + qexp) << 23),
                     [&](int r, int word, int part8, uint2 x) { sts64(q_at + swizzled(r, word, N) + part8 * 8, x.x, x.y); });
-      if (tid < 2 * R) S.base[tid / R][tid % R] = make_float2(S.qsum[tid % R], 0.f);
+      if (tid < R) S.base[tid / CR][tid % CR] = make_float4(S.qsum[tid % CR * 2], S.qsum[tid % CR * 2 + 1], 0.f, 0.f);
       if (tid == 0) S.bad[turn ^ 1] = S.qmax[turn ^ 1] = 0;
       fence_proxy_async();
       __syncthreads();
     }
     const float k_mul = P.scale * 16777216.f * __int_as_float((127 - query_exponent(S.qmax[turn])) << 23);
     const Gather G(P, b, h);
-    float l[CR], z[CR], up = 3e38f;  // sum of p, sum of p (y + 8 t) of this thread's positions; w = p t up
+    Two l[CR / 2], z[CR / 2];  // of two queries: sum of p, sum of p (y + 8 t) of this thread's positions
+    float up = 3e38f;          // the weights' power of two: w = p t up
 #pragma unroll
-    for (int r = 0; r < CR; ++r) l[r] = z[r] = 0.f;
+    for (int r = 0; r < CR / 2; ++r) l[r] = z[r] = two(0.f, 0.f);
 
     // half of the K codes of a stage's rows into tensor memory: two to a column, as the masks leave them
     auto k_codes = [&](int i) {
@@ -255,7 +273,7 @@ __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& par
       tm_after();
 #pragma unroll
       for (int kk = 0; kk < 8; ++kk)
-        mma_tmem(tm_s, tm_a + kk * 8, operand(q_at + (kk >> 2) * (N * 128) + (kk & 3) * 32, 16, 1024), shape_word(N, 0), kk > 0);
+        mma_tmem(tm_s, tm_a + kk * 8, q_op + ((kk >> 2) * (N * 128) + (kk & 3) * 32) / 16, shape_word(N, 0), kk > 0);
       if (!lost) mma_done(&S.s_bar[g]);
     };
     if (n_mine > 0) {
@@ -265,7 +283,7 @@ __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& par
       tm_before();
       named_bar_sync(1 + g, 256);
       // (test hook: the first scores of CTA 0 are never reported, so the bounded waits run out)
-      if (elected) start_scores(P.test_lose && blockIdx.x == 0 && at == part.first);
+      if (issues && elect()) start_scores(P.test_lose && blockIdx.x == 0 && at == part.first);
       __syncwarp();
     }
 
@@ -273,9 +291,8 @@ __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& par
     for (int i = 0; i < n_mine; ++i) {
       const uint32_t stage = ring_at + (i % kTcRing) * kTcStage;
       const bool more = i + 1 < n_mine;
-      const float2 kp = widen16(par0.x, P.half), vp = widen16(par0.y, P.half);
-      par0 = par1;
-      par1 = par2;
+      const float2 kp = widen16(par.x, P.half), vp = widen16(par.y, P.half);
+      par = scales(G, par_at1);  // of the next tile
       float x[CR];
       wait_for(&S.s_bar[g], s_turn++);
       tm_after();
@@ -286,23 +303,24 @@ __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& par
         __syncwarp();
         k_codes(i + 1);
       }
+      tm_wait_ld4(x);
 #pragma unroll
-      for (int c = 0; c < CR; c += 4) tm_wait_ld4(x + c);
+      for (int c = 4; c < CR; c += 4) tm_pass4(x + c);
       // scores from the running maximum on
       const float ks = kp.x * k_mul;
       float t = vp.x, y8 = fmaf(8.f, vp.x, vp.y), top = -INFINITY;
-      const float4* base = reinterpret_cast<const float4*>(S.base[g] + col0);
+      const float4* base = S.base[g] + col0 / 2;
 #pragma unroll
       for (int r = 0; r < CR; r += 2) {
         const float4 qm = base[r >> 1];
-        x[r] = fmaf(x[r], ks, fmaf(kp.y, qm.x, qm.y));
-        x[r + 1] = fmaf(x[r + 1], ks, fmaf(kp.y, qm.z, qm.w));
+        const float2 x2 = each(fma2(two(x[r], x[r + 1]), two(ks, ks), fma2(two(kp.y, kp.y), two(qm.x, qm.y), two(qm.z, qm.w))));
+        x[r] = x2.x, x[r + 1] = x2.y;
         top = fmaxf(top, fmaxf(x[r], x[r + 1]));
       }
       // what a query does not see: past the end, or behind it in the tail.  (A masked row may hold anything, and 0 NaN is
       // NaN: what a tail row's V scale would spoil, its scores spoil instead.)
-      const int pos = (seg0 + g + 2 * i) * kTile + key;
-      if ((seg0 + g + 2 * i + 1) * kTile > n_list) {
+      const int pos = index(i);
+      if (pos - key + kTile > n_list) {
         const bool spoilt = pos >= n_list && !(fabsf(t) <= FLT_MAX && fabsf(y8) <= FLT_MAX);
         if (spoilt) t = y8 = 0.f;
         top = -INFINITY;
@@ -316,7 +334,7 @@ __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& par
       // the maximum moves only where a score passes it by 2^8, the weights' scale where one passes 64
       tm_before();
       const bool raise = named_bar_or(3 + g, 256, top > 8.f || fabsf(t) * up > 64.f || i == 0);
-      if (elected && more) start_scores(false);
+      if (issues && more && elect()) start_scores(false);
       __syncwarp();
       if (raise) {
         const auto larger = [](float a, float c) { return fmaxf(a, c); };
@@ -341,7 +359,7 @@ __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& par
         }
 #pragma unroll
         for (int c = 0; c < CR; c += 4) {
-          float o[4];
+          float o[4], f[4], down[4];
           if (i > 0) {
             tm_ld4(o, tm_o + mine + col0 + c);
             tm_wait_ld4(o);
@@ -352,12 +370,20 @@ __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& par
             const float v = fmaxf(fmaxf(S.red[g][0][r][0], S.red[g][1][r][0]), fmaxf(S.red[g][2][r][0], S.red[g][3][r][0]));
             // (a query that sees nothing of the group's first tile sees nothing of the later ones)
             const float d = i == 0 ? (v == -INFINITY ? 0.f : v) : fmaxf(v, 0.f);
-            const float f = ex2(-d);
+            f[e] = ex2(-d);
             x[c + e] -= d;
-            l[c + e] *= f;
-            z[c + e] *= f;
-            o[e] *= f * scale_now;
-            if (key == r) S.base[g][r].y -= d;
+            o[e] *= f[e] * scale_now;
+            down[e] = d;
+          }
+#pragma unroll
+          for (int e = 0; e < 4; e += 2) {
+            l[(c + e) / 2] = mul2(l[(c + e) / 2], two(f[e], f[e + 1]));
+            z[(c + e) / 2] = mul2(z[(c + e) / 2], two(f[e], f[e + 1]));
+            if (key == (col0 + c + e) / 2) {
+              float4& of = S.base[g][(col0 + c + e) / 2];
+              of.z -= down[e];
+              of.w -= down[e + 1];
+            }
           }
           if (i > 0) tm_st4(tm_o + mine + col0 + c, o);
         }
@@ -369,7 +395,7 @@ __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& par
         tm_after();
       }
       {
-        const uint32_t row = stage + (kChunk + lane) * 32;
+        const uint32_t row = stage + (kChunk + lane) * 32, to = v_at + swizzled(key, 8 * half, kTile);
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
           const uint4 raw = lds128(row + ((c << 4) ^ swap));
@@ -377,39 +403,42 @@ __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& par
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             const uint32_t v = w[j] >> 8;
-            sts128(v_at + swizzled(key, 8 * half + 4 * c + j, kTile), minus(w[j] & 0x000f000fu, 0x00080008u),
+            sts128(to ^ ((4 * c + j) << 4), minus(w[j] & 0x000f000fu, 0x00080008u),
                    minus(w[j] & 0x00f000f0u, 0x00800080u), minus(v & 0x000f000fu, 0x00080008u), minus(v & 0x00f000f0u, 0x00800080u));
           }
         }
       }
       __syncwarp();  // the stage has been read
-      if (i + kTcRing < n_mine) par2 = fetch(G, i + kTcRing, pos_next, pg_next);
+      par_at1 = par_at2;
+      par_at2 = i + kTcRing < n_mine ? fetch(G, i + kTcRing, pos_next, pg_next) : ~0u;
       cp_commit();
       pos_next = pos_then;
-      pg_next = G.page(pos_then);
+      pg_next = page(G, i + kTcRing + 1, pos_then);
       pos_then = position(G, i + kTcRing + 2);
       // weights
       const float w_of = t * up;
 #pragma unroll
       for (int c = 0; c < CR; c += 4) {
-        float p[4];
+        uint32_t w[2];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          p[e] = ex2(x[c + e]);
-          l[c + e] += p[e];
-          z[c + e] = fmaf(p[e], y8, z[c + e]);
+        for (int e = 0; e < 4; e += 2) {
+          const Two p = two(ex2(x[c + e]), ex2(x[c + e + 1]));
+          l[(c + e) / 2] = add2(l[(c + e) / 2], p);
+          z[(c + e) / 2] = fma2(p, two(y8, y8), z[(c + e) / 2]);
+          const float2 w2 = each(mul2(p, two(w_of, w_of)));
+          w[e / 2] = pack_f16(w2.x, w2.y);
         }
         const int r = col0 + c;
-        sts64(w_at + key * 128 + (((r >> 3) ^ (key & 7)) << 4) + (r & 4) * 2, pack_f16(p[0] * w_of, p[1] * w_of), pack_f16(p[2] * w_of, p[3] * w_of));
+        sts64(w_at + key * 128 + (((r >> 3) ^ (key & 7)) << 4) + (r & 4) * 2, w[0], w[1]);
       }
       fence_proxy_async();
       tm_before();
       named_bar_sync(1 + g, 256);
-      if (elected) {
+      if (issues && elect()) {
         tm_after();
 #pragma unroll
         for (int kk = 0; kk < 8; ++kk)
-          mma_smem(tm_o, operand(v_at + kk * 2048, kTile * 128, 1024), operand(w_at + kk * 2048, 16384, 1024), shape_word(N, 1), i > 0 || kk > 0);
+          mma_smem(tm_o, v_op + kk * 2048 / 16, w_op + kk * 2048 / 16, shape_word(N, 1), kk > 0 ? 1 : i);
         mma_done(&S.o_bar[g]);
       }
       __syncwarp();
@@ -435,7 +464,9 @@ __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& par
     const auto add = [](float a, float c) { return a + c; };
 #pragma unroll
     for (int c = 0; c < CR; c += 4) {
-      const float ls = of_four(l + c, lane, add), zs = of_four(z + c, lane, add);
+      const float2 l0 = each(l[c / 2]), l1 = each(l[c / 2 + 1]), z0 = each(z[c / 2]), z1 = each(z[c / 2 + 1]);
+      const float l4[4] = {l0.x, l0.y, l1.x, l1.y}, z4[4] = {z0.x, z0.y, z1.x, z1.y};
+      const float ls = of_four(l4, lane, add), zs = of_four(z4, lane, add);
       if (lane < 4) S.red[g][wq][col0 + c + lane][0] = ls, S.red[g][wq][col0 + c + lane][1] = zs;
     }
     __syncthreads();  // both groups are done with their operands: records take their place
@@ -446,7 +477,7 @@ __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& par
       const float ls = (S.red[g][0][r][0] + S.red[g][1][r][0]) + (S.red[g][2][r][0] + S.red[g][3][r][0]);
       S.sums[g][r] = (S.red[g][0][r][1] + S.red[g][1][r][1]) + (S.red[g][2][r][1] + S.red[g][3][r][1]);
       float* rec = meet + (g * R + r) * kRowFloats;
-      rec[kKv4D] = ls == 0.f ? -FLT_MAX : -S.base[g][r].y;
+      rec[kKv4D] = ls == 0.f ? -FLT_MAX : -(r & 1 ? S.base[g][r >> 1].w : S.base[g][r >> 1].z);
       rec[kKv4D + 1] = ls;
     }
     named_bar_sync(1 + g, 256);
