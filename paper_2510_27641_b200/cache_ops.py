@@ -200,12 +200,12 @@ def kv4_verify(q: torch.Tensor, codes: torch.Tensor, params: torch.Tensor, kv_le
         assert (out.dtype is _F32 or out.dtype is q.dtype) and out.shape == shape and out.is_contiguous(), \
             "out: contiguous, of q's shape, of q's type or float32"
     if lse is None:
-        lse = torch.empty(rows, dtype=_F32, device=q.device)
+        lse = q.new_empty(rows, dtype=_F32)
         made.append(lse)
     else:
         assert lse.dtype is _F32 and lse.shape == rows and lse.is_contiguous()
     if workspace is None:
-        workspace = torch.empty((need,), dtype=torch.uint8, device=q.device)
+        workspace = q.new_empty(need // 2)   # (in the queries' 16-bit type)
         made.append(workspace)
         a.workspace_bytes = need
     else:
@@ -307,39 +307,32 @@ def evict(scores: torch.Tensor, kv_len: torch.Tensor, budget: int, *, n_sink: in
     made = []
 
     def new(shape):
-        made.append(torch.empty(shape, dtype=_I32, device=scores.device))
+        made.append(scores.new_empty(shape, dtype=_I32))
         return made[-1]
 
     if src is None:
         src = new(moves)
     if dst is None:
         dst = new(moves)
-    assert src.dtype is _I32 and src.is_contiguous() and src.shape == moves, "src: contiguous int32 [n_layers, B, G, moves]"
-    assert dst.dtype is _I32 and dst.is_contiguous() and dst.shape == moves, "dst: like src"
+    assert src.dtype is _I32 and src.shape == moves and src.is_contiguous(), "src: contiguous int32 [n_layers, B, G, moves]"
+    assert dst.dtype is _I32 and dst.shape == moves and dst.is_contiguous(), "dst: like src"
     if n_moves is None:
         n_moves = new(moves[:3])
     if new_len is None:
         new_len = new((b,))
-    a.scores, a.kv_len, a.seq_len = scores.data_ptr(), _ints(kv_len, b, "kv_len"), _ints(seq_len, b, "seq_len")
+    a.scores, a.kv_len = scores.data_ptr(), _ints(kv_len, b, "kv_len")
     a.src, a.dst = src.data_ptr(), dst.data_ptr()
-    a.n_moves, a.new_len = _ints(n_moves, moves[0] * b * moves[2], "n_moves"), _ints(new_len, b, "new_len")
-    a.positions, a.positions_out = _like_scores(positions, scores, _I32, "positions"), _like_scores(positions_out, scores, _I32, "positions_out")
-    a.scores_out = _like_scores(scores_out, scores, _F32, "scores_out")
+    a.seq_len = None if seq_len is None else _ints(seq_len, b, "seq_len")
+    a.n_moves = _ints(n_moves, moves[0] * b * moves[2], "n_moves")
+    a.new_len = _ints(new_len, b, "new_len")
+    a.positions = None if positions is None else _like_scores(positions, scores, _I32, "positions")
+    a.positions_out = None if positions_out is None else _like_scores(positions_out, scores, _I32, "positions_out")
+    a.scores_out = None if scores_out is None else _like_scores(scores_out, scores, _F32, "scores_out")
     _call("specattn_evict", ref, index, stream)
     if stream is not None:
         for t in made:
             t.record_stream(stream)
     return src, dst, n_moves, new_len
-
-
-def _addresses(ptrs, tensors):
-    """Tensors that differ in nothing but their address, by address."""
-    first = tensors[0]
-    shape, stride, dtype = first.shape, first.stride(), first.dtype
-    for i, t in enumerate(tensors):
-        assert t is first or (t.dtype is dtype and t.shape == shape and t.stride() == stride), "pools of one shape, type and strides expected"
-        ptrs[i] = t.data_ptr()
-    return shape, stride, dtype
 
 
 def move_rows(pools: Sequence[torch.Tensor], src: torch.Tensor, dst: torch.Tensor, n_moves: torch.Tensor, *,
@@ -355,11 +348,10 @@ def move_rows(pools: Sequence[torch.Tensor], src: torch.Tensor, dst: torch.Tenso
         return status
     assert params is None or len(params) == n
     index = _device(src, dst, n_moves, block_table, status, *pools, *(params or ()))
-    ptrs = (C.c_void_p * n)()
-    par_ptrs = None if params is None else (C.c_void_p * n)()
     pool, par = pools[0], None if params is None else params[0]
-    key = ("move", n, _addresses(ptrs, pools), None if params is None else _addresses(par_ptrs, params), src.shape, pages_per_seq,
-           None if block_table is None else (block_table.shape, block_table.dtype))
+    shape, strides, par_strides = pool.shape, pool.stride(), None if par is None else par.stride()
+    key = ("move", n, shape, strides, pool.dtype, src.shape, pages_per_seq, None if block_table is None else block_table.shape,
+           None if par is None else (par.shape, par_strides, par.dtype))
 
     def make():
         n_pages, two, page, heads, width = pool.shape
@@ -377,14 +369,22 @@ def move_rows(pools: Sequence[torch.Tensor], src: torch.Tensor, dst: torch.Tenso
             a.param_bytes = par.shape[4] * size
             a.pstride_page, a.pstride_kv, a.pstride_slot, a.pstride_head = [x * size for x in _strides(par, 0, 4)]
         a.block_table_stride, a.move_stride = _pages_per_seq(block_table, pages_per_seq, b), stride
-        return a, C.byref(a), b, b * g
+        ptrs, par_ptrs = (C.c_void_p * n)(), None if par is None else (C.c_void_p * n)()
+        a.pools, a.params = ptrs, par_ptrs
+        return a, C.byref(a), b, b * g, ptrs, par_ptrs
 
-    a, ref, b, lists = _calls.get(key, make)
+    a, ref, b, lists, ptrs, par_ptrs = _calls.get(key, make)
+    for i, t in enumerate(pools):
+        assert t is pool or (t.dtype is pool.dtype and t.shape == shape and t.stride() == strides), "pools of one shape, type and strides expected"
+        ptrs[i] = t.data_ptr()
+    if par is not None:
+        for i, t in enumerate(params):
+            assert t is par or (t.dtype is par.dtype and t.shape == par.shape and t.stride() == par_strides), "params of one shape, type and strides expected"
+            par_ptrs[i] = t.data_ptr()
     assert src.dtype is _I32 and src.is_contiguous()
     assert dst.dtype is _I32 and dst.is_contiguous() and dst.shape == src.shape
-    a.pools, a.params = ptrs, par_ptrs
     if block_table is not None:
-        assert block_table.is_contiguous()
+        assert block_table.dtype is _I32 and block_table.is_contiguous()
         a.block_table = block_table.data_ptr()
     a.src, a.dst, a.n_moves = src.data_ptr(), dst.data_ptr(), _ints(n_moves, lists, "n_moves")
     a.status = _ints(status, b, "status")

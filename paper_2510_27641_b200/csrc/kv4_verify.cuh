@@ -39,6 +39,9 @@ struct Kv4Params {
   int engine, test_lose;               // 1: mma.sync, 2: tcgen05, 0: by the lengths
 };
 
+// A value that all lanes share, in a register that the warp shares.
+__device__ __forceinline__ int uniform(int x) { return static_cast<int>(__reduce_or_sync(0xffffffffu, static_cast<unsigned>(x))); }
+
 // The units of a path: (sequence, KV head), once for every group of query rows.
 struct Units {
   int n, rows;  // units; query rows of one
@@ -228,9 +231,9 @@ struct Gather {
   int first_page;                       // without a table
 
   __device__ __forceinline__ Gather(const Kv4Params& p, int b, int h) : P(p) {
-    n_list = list_len(P, b, h);
+    n_list = uniform(list_len(P, b, h));
     n_all = n_list + P.tail;
-    ctx = max(0, P.kv_len[b]);
+    ctx = uniform(max(0, P.kv_len[b]));
     list = P.dense ? nullptr : P.idx + (static_cast<long long>(b) * P.G + (P.G > 1 ? h : 0)) * P.idx_stride;
     table = P.cache.table != nullptr ? P.cache.table + b * P.cache.table_stride : nullptr;
     first_page = static_cast<int>(min(b * P.cache.table_stride, P.cache.n_pages));  // (n_pages fits; beyond it no page is)

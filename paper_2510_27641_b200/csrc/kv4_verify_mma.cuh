@@ -52,19 +52,20 @@ struct MmaShared {
 template <int NT, int NWARP, int STAGES>
 __device__ __forceinline__ void mma_path(const Kv4Params& P, const Partition& part, unsigned char* smem, MmaShared<NT * 8>& S) {
   using K = MmaPath<NT, NWARP, STAGES>;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int tid = threadIdx.x, lane = tid & 31, warp = uniform(tid >> 5);
   const int g = lane >> 2, t = lane & 3;
   const uint32_t ring_at = smem_u32(smem + K::kQBytes + warp * K::kRing);
   const Units units = units_of(P, 0);
   const auto sync = [] { named_bar_sync(5, NWARP * 32); };  // (other warps of the CTA may have left)
-  int u = part.unit, u_start = part.start, turn = 0;
+  const int last = uniform(part.last);
+  int u = uniform(part.unit), u_start = uniform(part.start), turn = 0;
 
   // ---- one segment of a unit after the other ----
-  for (int at = part.first; at < part.last;) {
+  for (int at = uniform(part.first); at < last;) {
     const int rg = u / (P.B * P.H), bh = u - rg * P.B * P.H, b = bh / P.H, h = bh - b * P.H;
     const Gather G(P, b, h);
     const int n_list = G.n_list, n_chunks = (G.n_all + kChunk - 1) / kChunk;
-    const int seg0 = at - u_start, seg1 = min(n_chunks, part.last - u_start);  // chunks of the unit
+    const int seg0 = at - u_start, seg1 = min(n_chunks, last - u_start);  // chunks of the unit
     const int row0 = rg * units.rows, n_rows = min(units.rows, P.rows - row0);
 
     auto position = [&](int chunk) { return chunk < seg1 ? G.position(chunk * kChunk + lane) : 0; };
@@ -151,155 +152,142 @@ __device__ __forceinline__ void mma_path(const Kv4Params& P, const Partition& pa
       }
       const uint32_t stage = ring_at + ((chunk / NWARP) % STAGES) * kStageBytes;
 
-      // first product: scores of two tiles of 16 positions
-      float s[2][NT][4];
-#pragma unroll
-      for (int h2 = 0; h2 < 2; ++h2)
+      // two tiles of 16 positions, one after the other: a loop of both would not fit the instruction caches
+#pragma unroll 1
+      for (int h2 = 0; h2 < 2; ++h2) {
+        // first product
+        const uint32_t k_row = stage + (h2 * 16 + g) * kKv4Row + t * 16;
+        float s[NT][4];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) s[h2][nt][e] = 0.f;
-      {
-        uint32_t ka[2][2][4];
+          for (int e = 0; e < 4; ++e) s[nt][e] = 0.f;
+        {
+          const uint4 k0 = lds128(k_row), k1 = lds128(k_row + 8 * kKv4Row);
+          const uint32_t ka[2][4] = {{k0.x, k0.y, k0.z, k0.w}, {k1.x, k1.y, k1.z, k1.w}};
 #pragma unroll
-        for (int h2 = 0; h2 < 2; ++h2)
+          for (int w = 0; w < 4; ++w)
 #pragma unroll
-          for (int r = 0; r < 2; ++r) {
-            const uint4 x = lds128(stage + (h2 * 16 + r * 8 + g) * kKv4Row + t * 16);
-            ka[h2][r][0] = x.x, ka[h2][r][1] = x.y, ka[h2][r][2] = x.z, ka[h2][r][3] = x.w;
+            for (int hi = 0; hi < 2; ++hi) {
+              const uint32_t x0 = hi ? ka[0][w] >> 8 : ka[0][w], x1 = hi ? ka[1][w] >> 8 : ka[1][w];
+              const uint32_t a0 = x0 & 0x000f000fu, a1 = x1 & 0x000f000fu, a2 = x0 & 0x00f000f0u, a3 = x1 & 0x00f000f0u;
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) {
+                const uint2 qb = q_op[(nt * 8 + 2 * w + hi) * 32];
+                mma_f16(s[nt], a0, a1, a2, a3, qb.x, qb.y);
+              }
+            }
+        }
+
+        // scales: (s, z) and (t, y) of the positions g and g + 8; scores from the running maximum on
+        float t_of[2], y_of[2];
+        {
+          const uint32_t at_par = stage + 2 * kChunk * kKv4Row + (h2 * 16 + g) * 8;
+          const uint2 raw[2] = {lds64(at_par), lds64(at_par + 64)};
+          float2 kp[2], vp[2];
+          if (P.half) {
+#pragma unroll
+            for (int r = 0; r < 2; ++r) kp[r] = widen<true>(raw[r].x), vp[r] = widen<true>(raw[r].y);
+          } else {
+#pragma unroll
+            for (int r = 0; r < 2; ++r) kp[r] = widen<false>(raw[r].x), vp[r] = widen<false>(raw[r].y);
           }
 #pragma unroll
-        for (int w = 0; w < 4; ++w)
-#pragma unroll
-          for (int hi = 0; hi < 2; ++hi) {
-            uint32_t a[2][4];
-#pragma unroll
-            for (int h2 = 0; h2 < 2; ++h2) {
-              const uint32_t x0 = hi ? ka[h2][0][w] >> 8 : ka[h2][0][w], x1 = hi ? ka[h2][1][w] >> 8 : ka[h2][1][w];
-              a[h2][0] = x0 & 0x000f000fu, a[h2][1] = x1 & 0x000f000fu;
-              a[h2][2] = x0 & 0x00f000f0u, a[h2][3] = x1 & 0x00f000f0u;
-            }
+          for (int r = 0; r < 2; ++r) {
+            const float ks = kp[r].x * k_mul;
+            t_of[r] = vp[r].x;
+            y_of[r] = fmaf(8.f, vp[r].x, vp[r].y);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-              const uint2 qb = q_op[(nt * 8 + 2 * w + hi) * 32];
-#pragma unroll
-              for (int h2 = 0; h2 < 2; ++h2) mma_f16(s[h2][nt], a[h2][0], a[h2][1], a[h2][2], a[h2][3], qb.x, qb.y);
+              const float2 x2 = each(fma2(two(s[nt][2 * r], s[nt][2 * r + 1]), two(ks, ks), fma2(two(kp[r].y, kp[r].y), sq[nt], m[nt])));
+              s[nt][2 * r] = x2.x, s[nt][2 * r + 1] = x2.y;
             }
           }
-      }
-
-      // scales: (s, z) and (t, y) of the positions g and g + 8 of both tiles; scores from the running maximum on
-      float t_of[2][2], y_of[2][2], t_max = 0.f;
-#pragma unroll
-      for (int h2 = 0; h2 < 2; ++h2)
-#pragma unroll
-        for (int r = 0; r < 2; ++r) {
-          const uint2 x = lds64(stage + 2 * kChunk * kKv4Row + (h2 * 16 + r * 8 + g) * 8);
-          const float2 kp = widen16(x.x, P.half), vp = widen16(x.y, P.half);
-          const float ks = kp.x * k_mul;
-          t_of[h2][r] = vp.x;
-          y_of[h2][r] = fmaf(8.f, vp.x, vp.y);
-          t_max = fmaxf(t_max, fabsf(vp.x));
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            const float2 x2 = each(fma2(two(s[h2][nt][2 * r], s[h2][nt][2 * r + 1]), two(ks, ks), fma2(two(kp.y, kp.y), sq[nt], m[nt])));
-            s[h2][nt][2 * r] = x2.x, s[h2][nt][2 * r + 1] = x2.y;
-          }
         }
-      // what a query does not see: past the end, or behind it in the tail.  (A masked row may hold anything, and 0 NaN is
-      // NaN: what a tail row's V scale would spoil, its scores spoil instead.)
-      const int i0 = chunk * kChunk;
-      if (i0 + kChunk > n_list) {
-#pragma unroll
-        for (int h2 = 0; h2 < 2; ++h2)
+        // what a query does not see: past the end, or behind it in the tail.  (A masked row may hold anything, and 0 NaN is
+        // NaN: what a tail row's V scale would spoil, its scores spoil instead.)
+        const int i0 = chunk * kChunk + h2 * 16;
+        if (__builtin_expect(i0 + 16 > n_list, 0)) {
 #pragma unroll
           for (int r = 0; r < 2; ++r) {
-            const int i = i0 + h2 * 16 + r * 8 + g;
-            const bool spoilt = i >= n_list && !(fabsf(t_of[h2][r]) <= FLT_MAX && fabsf(y_of[h2][r]) <= FLT_MAX);
-            if (spoilt) t_of[h2][r] = y_of[h2][r] = 0.f;
+            const int i = i0 + r * 8 + g;
+            const bool spoilt = i >= n_list && !(fabsf(t_of[r]) <= FLT_MAX && fabsf(y_of[r]) <= FLT_MAX);
+            if (spoilt) t_of[r] = y_of[r] = 0.f;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
               for (int e = 0; e < 2; ++e) {
-                if (spoilt) s[h2][nt][2 * r + e] = NAN;
-                if (i >= n_list + S.limit[nt * 8 + 2 * t + e]) s[h2][nt][2 * r + e] = -INFINITY;
+                if (spoilt) s[nt][2 * r + e] = NAN;
+                if (i >= n_list + S.limit[nt * 8 + 2 * t + e]) s[nt][2 * r + e] = -INFINITY;
               }
           }
-      }
-      // the maximum moves only where a score passes it by 2^8, the weights' scale where one passes 64
-      float top = s[0][0][0];
-#pragma unroll
-      for (int h2 = 0; h2 < 2; ++h2)
+        }
+        // the maximum moves only where a score passes it by 2^8, the weights' scale where one passes 64
+        float top = s[0][0], t_max = fmaxf(fabsf(t_of[0]), fabsf(t_of[1]));
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) top = fmaxf(top, s[h2][nt][e]);
-      if (__any_sync(0xffffffffu, top > 8.f || t_max * up > 64.f || chunk == first)) {
-        t_max = t_max <= FLT_MAX ? t_max : 0.f;
+          for (int e = 0; e < 4; ++e) top = fmaxf(top, s[nt][e]);
+        const bool begins = chunk == first && h2 == 0;
+        if (__builtin_expect(__any_sync(0xffffffffu, top > 8.f || t_max * up > 64.f || begins), 0)) {
+          t_max = t_max <= FLT_MAX ? t_max : 0.f;
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) t_max = fmaxf(t_max, __shfl_xor_sync(0xffffffffu, t_max, o));
-        // t_max up in [32, 64)
-        float up_now = up;
-        if (t_max > 0.f) up_now = fminf(up, __int_as_float((127 + min(5 + 127 - (__float_as_int(t_max) >> 23), 100)) << 23));
-        const float scale_now = up_now / up;
-        up = up_now;
+          for (int o = 16; o > 0; o >>= 1) t_max = fmaxf(t_max, __shfl_xor_sync(0xffffffffu, t_max, o));
+          // t_max up in [32, 64)
+          float up_now = up;
+          if (t_max > 0.f) up_now = fminf(up, __int_as_float((127 + min(5 + 127 - (__float_as_int(t_max) >> 23), 100)) << 23));
+          const float scale_now = up_now / up;
+          up = up_now;
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          float f[2], down[2];
+          for (int nt = 0; nt < NT; ++nt) {
+            float f[2], down[2];
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            float v = fmaxf(fmaxf(s[0][nt][e], s[0][nt][2 + e]), fmaxf(s[1][nt][e], s[1][nt][2 + e]));
-            v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 4));
-            v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 8));
-            v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 16));
-            // (a query that sees nothing of the warp's first chunk sees nothing of the later ones)
-            const float d = chunk == first ? (v == -INFINITY ? 0.f : v) : fmaxf(v, 0.f);
-            f[e] = ex2(-d);
-            down[e] = d;
-            s[0][nt][e] -= d, s[0][nt][2 + e] -= d, s[1][nt][e] -= d, s[1][nt][2 + e] -= d;
-          }
-          m[nt] = add2(m[nt], two(-down[0], -down[1]));
-          l[nt] = mul2(l[nt], two(f[0], f[1]));
-          y[nt] = mul2(y[nt], two(f[0], f[1]));
+            for (int e = 0; e < 2; ++e) {
+              float v = fmaxf(s[nt][e], s[nt][2 + e]);
+              v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 4));
+              v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 8));
+              v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 16));
+              // (a query that sees nothing of the warp's first tile sees nothing of the later ones)
+              const float d = begins ? (v == -INFINITY ? 0.f : v) : fmaxf(v, 0.f);
+              f[e] = ex2(-d);
+              down[e] = d;
+              s[nt][e] -= d, s[nt][2 + e] -= d;
+            }
+            m[nt] = add2(m[nt], two(-down[0], -down[1]));
+            l[nt] = mul2(l[nt], two(f[0], f[1]));
+            y[nt] = mul2(y[nt], two(f[0], f[1]));
 #pragma unroll
-          for (int e = 0; e < 2; ++e) f[e] = chunk == first ? 0.f : f[e] * scale_now;
+            for (int e = 0; e < 2; ++e) f[e] = begins ? 0.f : f[e] * scale_now;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            acc8[nt][e] *= f[e & 1];
+            for (int e = 0; e < 4; ++e) {
+              acc8[nt][e] *= f[e & 1];
 #pragma unroll
-            for (int mt = 0; mt < 8; ++mt) acc[mt][nt][e] *= f[e & 1];
+              for (int mt = 0; mt < 8; ++mt) acc[mt][nt][e] *= f[e & 1];
+            }
           }
         }
-      }
 
-      // weights, and the second product
-#pragma unroll
-      for (int h2 = 0; h2 < 2; ++h2) {
+        // weights, and the second product
         uint32_t pb[NT][2];
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-          const float w_of = h2 ? -t_of[h2][r] * up : t_of[h2][r] * up;
+          const float w_of = h2 ? -t_of[r] * up : t_of[r] * up;
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
-            const Two p = two(ex2(s[h2][nt][2 * r]), ex2(s[h2][nt][2 * r + 1]));
+            const Two p = two(ex2(s[nt][2 * r]), ex2(s[nt][2 * r + 1]));
             l[nt] = add2(l[nt], p);
-            y[nt] = fma2(p, two(y_of[h2][r], y_of[h2][r]), y[nt]);
+            y[nt] = fma2(p, two(y_of[r], y_of[r]), y[nt]);
             const float2 w = each(mul2(p, two(w_of, w_of)));
             pb[nt][r] = transpose8(pack_f16(w.x, w.y));
           }
         }
         // V rows of positions 2 t, 2 t + 1, 2 t + 8, 2 t + 9 of the tile, 8 bytes to a lane
-        uint2 v[4];
+        const uint32_t v_row = stage + (kChunk + h2 * 16 + t) * kKv4Row + ((g * 8) ^ ((t & 2) << 4));
+        const uint2 v[4] = {lds64(v_row), lds64(v_row + 4 * kKv4Row), lds64(v_row + 8 * kKv4Row), lds64(v_row + 12 * kKv4Row)};
+        const uint32_t flip = h2 ? 0xffffffffu : 0u;
+        const uint32_t mid = h2 ? 0x80078007u : 0x80088008u;  // -7 (of -w: 15 w - 8 w), -8
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const int row = h2 * 16 + (k >> 1) * 8 + (k & 1) * 4 + t;
-          v[k] = lds64(stage + (kChunk + row) * kKv4Row + ((g * 8) ^ ((row & 2) << 4)));
-        }
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          const uint32_t mid = h2 ? 0x80078007u : 0x80088008u;  // -7 (of -w: 15 w - 8 w), -8
-          mma_f16(acc8[nt], mid, mid, mid, mid, pb[nt][0], pb[nt][1]);
-        }
+        for (int nt = 0; nt < NT; ++nt) mma_f16(acc8[nt], mid, mid, mid, mid, pb[nt][0], pb[nt][1]);
 #pragma unroll
         for (int w = 0; w < 2; ++w)
 #pragma unroll
@@ -310,9 +298,9 @@ __device__ __forceinline__ void mma_path(const Kv4Params& P, const Partition& pa
 #pragma unroll
             for (int hi = 0; hi < 2; ++hi) {
               const int mt = w * 4 + half * 2 + hi;
-              if (hi) x0 >>= 8, x1 >>= 8;
-              const uint32_t z0 = h2 ? ~x0 : x0, z1 = h2 ? ~x1 : x1;
-              const uint32_t a0 = z0 & 0x000f000fu, a1 = z0 & 0x00f000f0u, a2 = z1 & 0x000f000fu, a3 = z1 & 0x00f000f0u;
+              const uint32_t z0 = hi ? x0 >> 8 : x0, z1 = hi ? x1 >> 8 : x1;
+              const uint32_t a0 = (z0 ^ flip) & 0x000f000fu, a1 = (z0 ^ flip) & 0x00f000f0u, a2 = (z1 ^ flip) & 0x000f000fu,
+                             a3 = (z1 ^ flip) & 0x00f000f0u;
 #pragma unroll
               for (int nt = 0; nt < NT; ++nt) mma_f16(acc[mt][nt], a0, a1, a2, a3, pb[nt][0], pb[nt][1]);
             }
@@ -368,7 +356,7 @@ __device__ __forceinline__ void mma_path(const Kv4Params& P, const Partition& pa
       u_start += n_chunks;
       do {
         ++u;
-      } while (u < units.n && at < part.last && chunks_of(P, u, kChunk) == 0);
+      } while (u < units.n && at < last && chunks_of(P, u, kChunk) == 0);
     }
   }
 }

@@ -135,7 +135,7 @@ __device__ __forceinline__ float of_four(const float* in, int lane, Op op) {
 template <int R8>
 __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& part, unsigned char* smem_raw, Tc4Shared& S) {
   constexpr int R = R8 * 8, N = (R8 + 1) / 2 * 16, CR = R / 2;  // query rows; columns of the products; a thread's columns
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int tid = threadIdx.x, lane = tid & 31, warp = uniform(tid >> 5);
   // group; half of a row's codes and of the queries; quarter of a tile; position of a tile = lane of tensor memory
   const int g = warp >> 3, half = (warp >> 2) & 1, wq = warp & 3, key = wq * 32 + lane, col0 = half * CR;
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
@@ -161,16 +161,17 @@ __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& par
   tm_before();
   __syncthreads();
   tm_after();
-  const uint32_t tm_a = S.tmem + g * 192, tm_s = tm_a + 64, tm_o = tm_a + 128, mine = static_cast<uint32_t>(wq * 32) << 16;
+  const uint32_t tm_a = static_cast<uint32_t>(uniform(S.tmem)) + g * 192, tm_s = tm_a + 64, tm_o = tm_a + 128, mine = static_cast<uint32_t>(wq * 32) << 16;
   const uint64_t q_op = operand(q_at, 16, 1024), v_op = operand(v_at, kTile * 128, 1024), w_op = operand(w_at, 16384, 1024);
-  const bool issues = (__shfl_sync(0xffffffffu, warp, 0) & 7) == 0;  // a warp of each group
+  const bool issues = (warp & 7) == 0;  // a warp of each group
   uint32_t s_turn = 0, o_turn = 0;  // completions of this group's products that have been waited for
   auto wait_for = [&](unsigned long long* bar, uint32_t turn) {
     if (!mbar_wait(bar, turn & 1u, &S.abort)) S.abort = 1;
   };
   const uint32_t swap = ((lane >> 2) & 1) << 4;  // raw half rows of 32 bytes: halves swapped so that 8 lanes meet all banks
 
-  int u = part.unit, u_start = part.start, turn = 0;
+  const int last = uniform(part.last);
+  int u = uniform(part.unit), u_start = uniform(part.start), turn = 0;
   int b = 0, h = 0, seg0 = 0, seg1 = 0, n_tiles = 0, n_mine = 0, n_list = 0;
   int pos_next = 0, pg_next = -2, pos_then = 0;  // of this group's tile i + 3, of the one behind it
   uint32_t par_at1 = ~0u, par_at2 = ~0u;           // where its scales lie: of tiles i + 1, i + 2
@@ -209,7 +210,7 @@ __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& par
     n_list = G.n_list;
     n_tiles = (G.n_all + kTile - 1) / kTile;
     seg0 = at - u_start;
-    seg1 = min(n_tiles, part.last - u_start);
+    seg1 = min(n_tiles, last - u_start);
     n_mine = max(0, (seg1 - seg0 - g + 1) >> 1);  // tiles seg0 + g, seg0 + g + 2, ...
     int pos[kTcRing + 2], pg[kTcRing + 1];
 #pragma unroll
@@ -227,9 +228,10 @@ __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& par
     pg_next = pg[3];
     pos_then = pos[4];
   };
-  if (part.first < part.last) begin(part.first);
+  const int start_at = uniform(part.first);
+  if (start_at < last) begin(start_at);
 
-  for (int at = part.first; at < part.last;) {
+  for (int at = start_at; at < last;) {
     // ---- queries ----
     {
       Queries<kTcWarps, R> queries;
@@ -283,7 +285,7 @@ __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& par
       tm_before();
       named_bar_sync(1 + g, 256);
       // (test hook: the first scores of CTA 0 are never reported, so the bounded waits run out)
-      if (issues && elect()) start_scores(P.test_lose && blockIdx.x == 0 && at == part.first);
+      if (issues && elect()) start_scores(P.test_lose && blockIdx.x == 0 && at == start_at);
       __syncwarp();
     }
 
@@ -320,7 +322,7 @@ __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& par
       // what a query does not see: past the end, or behind it in the tail.  (A masked row may hold anything, and 0 NaN is
       // NaN: what a tail row's V scale would spoil, its scores spoil instead.)
       const int pos = index(i);
-      if (pos - key + kTile > n_list) {
+      if (__builtin_expect(pos - key + kTile > n_list, 0)) {
         const bool spoilt = pos >= n_list && !(fabsf(t) <= FLT_MAX && fabsf(y8) <= FLT_MAX);
         if (spoilt) t = y8 = 0.f;
         top = -INFINITY;
@@ -336,7 +338,7 @@ __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& par
       const bool raise = named_bar_or(3 + g, 256, top > 8.f || fabsf(t) * up > 64.f || i == 0);
       if (issues && more && elect()) start_scores(false);
       __syncwarp();
-      if (raise) {
+      if (__builtin_expect(raise, 0)) {
         const auto larger = [](float a, float c) { return fmaxf(a, c); };
 #pragma unroll
         for (int c = 0; c < CR; c += 4) {
@@ -453,10 +455,10 @@ __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& par
       u_start += n_tiles;
       do {
         ++u;
-      } while (u < units.n && at < part.last && chunks_of(P, u, kTile) == 0);
+      } while (u < units.n && at < last && chunks_of(P, u, kTile) == 0);
     }
     turn ^= 1;
-    if (at < part.last) begin(at);
+    if (at < last) begin(at);
     if (this_mine > 0) {
       wait_for(&S.o_bar[g], o_turn++);
       tm_after();
