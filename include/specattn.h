@@ -500,8 +500,8 @@ int specattn_kv4_read(const specattn_kv4_rows_args* args, void* cuda_stream);
  * Requirements: head_dim == 128; n_q * (n_q_heads / n_kv_heads) <= 64; batch * n_kv_heads <= 2048; lists
  * and, where dense, block_table_stride * page_size of at most 2^23 positions.
  * flags: SPECATTN_VERIFY_ENGINE_MMA_SYNC or SPECATTN_VERIFY_ENGINE_TCGEN05 forces one of two implementations of the same
- * operation.  With neither the kernel itself picks by the lengths that it finds: tcgen05 where they fill the GPU.  Results
- * agree within the tolerance of the operation either way.
+ * operation; TCGEN05 runs 17 to 48 query rows (SPECATTN_ERR_UNSUPPORTED otherwise).  With neither the kernel itself picks, by
+ * the rows and by the lengths that it finds.  Results agree within the tolerance of the operation either way.
  * workspace: specattn_kv4_verify_workspace_bytes() bytes, 256-byte aligned, no preparation and no
  * state between calls; two calls that may overlap on the GPU need separate ones.
  * (The call signals programmatic launch completion early: it does not count as the launch in front of a

@@ -33,26 +33,30 @@ int device_sm_count();
 
 namespace {
 
-constexpr int kThreads = 512;
-
-// What a call of R8 * 8 query rows runs with on mma.sync.
+// What a call of R8 * 8 query rows runs with.
+//
+// mma.sync: as many warps as hold a warp's output in registers.  tcgen05: sixteen warps of 128 registers, for 17 to 48 rows.
+// Below, dequantising is all there is to do, and mma.sync does it with fewer steps (8 sequences x 8 heads x 32768 positions, 4
+// / 16 query rows: 77 / 106 us against 119 / 126); above, sums do not fit (64 rows: 290 against 344).  Between, tcgen05 is
+// ahead from `kTensorLeast` chunks of 32 positions to a CTA on (the same positions, 24 / 32 / 40 rows: 137 / 149 / 158 us
+// against 145 / 168 / 249; 8 x 8 x 1200 positions, 16 chunks: 19.3 / 21.4 / 23.7 against 19.1 / 21.9 / 24.3).
 template <int R8>
 struct Config {
-  static constexpr int kGroups = R8 > 4 ? 2 : 1;               // of query rows: 32 are as many as registers hold
+  static constexpr int kGroups = R8 > 4 ? 2 : 1;               // of query rows, on mma.sync: 32 are as many as registers hold
   static constexpr int kTiles = (R8 + kGroups - 1) / kGroups;  // of eight queries
-  // Sixteen warps while 128 registers hold a warp's output; else eight take the registers of the others.
-  static constexpr int kWarps = R8 == 1 ? 16 : 8;
-  static constexpr int kStages = R8 == 1 ? 3 : 4;
+  static constexpr bool kTensor = R8 >= 3 && R8 <= 6;
+  static constexpr int kWarps = R8 == 1 ? 16 : R8 == 2 ? 12 : 8;
+  static constexpr int kStages = R8 <= 2 ? 3 : 4;
+  static constexpr int kThreads = kTensor ? kTcWarps * 32 : kWarps * 32;
   using Mma = MmaPath<kTiles, kWarps, kStages>;
-  static constexpr int kSmem = kTcSmem > Mma::kSmem ? kTcSmem : Mma::kSmem;
+  static constexpr int kSmem = kTensor && kTcSmem > Mma::kSmem ? kTcSmem : Mma::kSmem;
 };
+// Where both paths are there, a call on mma.sync gives eight of the sixteen warps' registers to the others.
 constexpr int kLaunchRegisters = 128, kMoreRegisters = 232, kFewRegisters = 24;
 static_assert(kMoreRegisters + kFewRegisters == 2 * kLaunchRegisters, "eight warps give what eight take");
 
-constexpr int kTensorLeast = 64;  // chunks of 32 positions to a CTA from which on tcgen05 is ahead
-
 template <int R8>
-__global__ void __launch_bounds__(kThreads, 1) kv4_verify_kernel(const __grid_constant__ Kv4Params P) {
+__global__ void __launch_bounds__(Config<R8>::kThreads, 1) kv4_verify_kernel(const __grid_constant__ Kv4Params P) {
   using C = Config<R8>;
   extern __shared__ __align__(1024) unsigned char smem[];
   __shared__ PartitionShared ps;
@@ -62,29 +66,33 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_verify_kernel(const __grid_co
     __device__ Shared() {}
   } sh;
   pdl_wait();  // everything below reads what earlier kernels may have written
-  bool tensor = P.engine == 2;
-  if (P.engine == 0) {
-    const int units = units_of(P, 1).n;
-    int mine = 0, total;
-    for (int u = threadIdx.x; u < units; u += kThreads) mine += chunks_of(P, u, kChunk);
-    scan<kThreads>(mine, ps, &total);
-    tensor = total >= kTensorLeast * static_cast<int>(gridDim.x);
-  }
-  if (tensor) {
-    const Partition part = cut<kThreads>(P, 1, kTile, 2, 12, ps);
-    tc_path<R8>(P, part, smem, sh.tc);
-  } else {
-    if (threadIdx.x < 2) sh.mma.bad[threadIdx.x] = sh.mma.qmax[threadIdx.x] = 0;
-    const Partition part = cut<kThreads>(P, 0, kChunk, C::kWarps, 32, ps);
-    if constexpr (C::kWarps * 32 < kThreads) {
-      if (threadIdx.x >= C::kWarps * 32) {
-        set_max_registers_dec<kFewRegisters>();
-        return;
-      }
-      set_max_registers_inc<kMoreRegisters>();
+  if constexpr (C::kTensor) {
+    constexpr int kTensorLeast = R8 == 3 ? 96 : R8 == 4 ? 0 : 16;
+    bool tensor = P.engine == 2 || (P.engine == 0 && kTensorLeast == 0);
+    if (P.engine == 0 && kTensorLeast > 0) {
+      const int units = units_of(P, 1).n;
+      int mine = 0, total;
+      for (int u = threadIdx.x; u < units; u += C::kThreads) mine += chunks_of(P, u, kChunk);
+      scan<C::kThreads>(mine, ps, &total);
+      tensor = total >= kTensorLeast * static_cast<int>(gridDim.x);
     }
-    mma_path<C::kTiles, C::kWarps, C::kStages>(P, part, smem, sh.mma);
+    if (tensor) {
+      const Partition part = cut<C::kThreads>(P, 1, kTile, 2, 12, ps);
+      tc_path<R8>(P, part, smem, sh.tc);
+      pdl_launch_dependents();
+      return;
+    }
   }
+  if (threadIdx.x < 2) sh.mma.bad[threadIdx.x] = sh.mma.qmax[threadIdx.x] = 0;
+  const Partition part = cut<C::kThreads>(P, 0, kChunk, C::kWarps, 32, ps);
+  if constexpr (C::kTensor) {
+    if (threadIdx.x >= C::kWarps * 32) {
+      set_max_registers_dec<kFewRegisters>();
+      return;
+    }
+    set_max_registers_inc<kMoreRegisters>();
+  }
+  mma_path<C::kTiles, C::kWarps, C::kStages>(P, part, smem, sh.mma);
   pdl_launch_dependents();
 }
 
@@ -168,6 +176,8 @@ int validate(const specattn_kv4_verify_args* args) {
   if (A.head_dim != kKv4D || A.n_q > SPECATTN_MAX_QUERY_ROWS || A.n_q * (A.n_q_heads / A.n_kv_heads) > SPECATTN_MAX_QUERY_ROWS ||
       static_cast<long long>(A.batch) * A.n_kv_heads > kMaxUnits)
     return SPECATTN_ERR_UNSUPPORTED;
+  const int rows = A.n_q * (A.n_q_heads / A.n_kv_heads);
+  if ((A.flags & SPECATTN_VERIFY_ENGINE_TCGEN05) && (rows <= 16 || rows > 48)) return SPECATTN_ERR_UNSUPPORTED;
   return SPECATTN_OK;
 }
 
@@ -191,7 +201,7 @@ int launch(const Kv4Params& P, int sms, cudaStream_t stream) {
   if (!((prepared.load(std::memory_order_acquire) >> dev) & 1ull)) {
     // (what one half of the warps gives the other takes: with fewer registers at launch they would wait for ever)
     cudaFuncAttributes built;
-    if (cudaFuncGetAttributes(&built, kv4_verify_kernel<R8>) != cudaSuccess || built.numRegs != kLaunchRegisters ||
+    if (cudaFuncGetAttributes(&built, kv4_verify_kernel<R8>) != cudaSuccess || (C::kTensor && built.numRegs != kLaunchRegisters) ||
         cudaFuncSetAttribute(kv4_verify_kernel<R8>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem) != cudaSuccess) {
       cudaGetLastError();
       return SPECATTN_ERR_CUDA;
@@ -201,7 +211,7 @@ int launch(const Kv4Params& P, int sms, cudaStream_t stream) {
   cudaLaunchConfig_t cfg;
   memset(&cfg, 0, sizeof(cfg));
   cfg.gridDim = dim3(sms);
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3(C::kThreads);
   cfg.dynamicSmemBytes = C::kSmem;
   cfg.stream = stream;
   cudaLaunchAttribute attr[1];

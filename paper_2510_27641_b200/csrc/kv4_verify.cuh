@@ -116,9 +116,11 @@ __device__ __forceinline__ int chunks_of(const Kv4Params& P, int u, int chunk) {
   return (list_len(P, b, bh - b * P.H) + P.tail + chunk - 1) / chunk;
 }
 
+constexpr int kMostParted = 256;  // units that may be cut into equal parts
 struct PartitionShared {
   int scan[33];
-  int unit, unit_start, total, length;
+  int unit, unit_start, first, last;
+  int chunks[kMostParted], parts[16];
 };
 // The units' chunks of `chunk` positions in a row, cut: this CTA's run is [first, last), its first unit `unit` begins
 // at chunk `start`.
@@ -157,51 +159,52 @@ __device__ __forceinline__ int scan(int v, PartitionShared& S, int* total) {
 
 // Two ways to cut.  Equal runs of all chunks, wherever units begin and end: every CTA does the same work, but one that meets
 // the end of a unit pays for the start of the next (`afresh`: as many chunks as take as long).  Or, where there are CTAs
-// enough, equal parts of units: the shortest length for which the parts are no more than the CTAs is searched for, and
-// taken if it exceeds an equal run by less than that.
+// enough, equal parts of units: of lengths from an equal run's on, in steps of an eighth, each tried by a warp, the
+// shortest whose parts are no more than the CTAs, if it exceeds an equal run by less than `afresh`.
 template <int kThreads>
 __device__ __forceinline__ Partition cut(const Kv4Params& P, int tensor, int chunk, int least, int afresh, PartitionShared& S) {
-  const int tid = threadIdx.x, grid = static_cast<int>(gridDim.x), units = units_of(P, tensor).n;
+  static_assert(kThreads >= kMostParted && kThreads <= 512, "a unit to a thread, a length to a warp");
+  const int tid = threadIdx.x, lane = tid & 31, grid = static_cast<int>(gridDim.x), units = units_of(P, tensor).n;
   const int per_thread = (units + kThreads - 1) / kThreads;
   const int u0 = min(tid * per_thread, units), u1 = min(u0 + per_thread, units);
   int mine = 0, total;
   for (int u = u0; u < u1; ++u) mine += chunks_of(P, u, chunk);
+  if (tid < kMostParted) S.chunks[tid] = mine;  // (read where a thread has one unit)
+  if (tid == 0) S.unit = units;
   const int before = scan<kThreads>(mine, S, &total);
   Partition p;
   p.unit = units;
   p.start = p.first = p.last = 0;
+  if (blockIdx.x == 0 && tid == 0) *P.path = tensor;
   const int per = max((total + grid - 1) / grid, least);
-  if (tid == 0) S.unit = units;
-  __syncthreads();
-  if (units <= grid && units <= kThreads) {  // (a unit to a thread)
-    // parts of at most `length` chunks, the length doubled in quarters until they fit
-    int length = per, count = 0, k = 0;
-    for (int step = 0; step < 32; ++step) {
-      k = (mine + length - 1) / length;
-      int all;
-      const int at = scan<kThreads>(k, S, &all);
-      if (all <= grid || length - per >= afresh) {
-        if (all > grid) break;
-        count = all;
-        // this thread's unit goes to CTAs at ... at + k - 1
-        if (tid < units) {
-          if (blockIdx.x == 0) P.parts[tid] = make_int2(k > 0 ? at : 0, at + k - 1 - (k > 0 ? 0 : at));
-          const int j = static_cast<int>(blockIdx.x) - at;
-          if (j >= 0 && j < k) {
-            S.unit = tid;
-            S.unit_start = before;
-            S.total = before + static_cast<int>(static_cast<long long>(mine) * j / k);
-            S.length = before + static_cast<int>(static_cast<long long>(mine) * (j + 1) / k);
-          }
-        }
-        break;
-      }
-      length += max(1, length / 8);
+  if (units <= min(grid, kMostParted)) {
+    const auto length_of = [&](int step) { return per + per * step / 8; };
+    {
+      const int warp = tid >> 5;
+      int n = 0;
+      for (int u = lane; u < units; u += 32) n += (S.chunks[u] + length_of(warp) - 1) / length_of(warp);
+      n = __reduce_add_sync(0xffffffffu, n);
+      if (lane == 0) S.parts[warp] = n;
     }
     __syncthreads();
-    if (count > 0 || total == 0) {
-      if (S.unit < units) p.unit = S.unit, p.start = S.unit_start, p.first = S.total, p.last = S.length;
-      if (blockIdx.x == 0 && tid == 0) *P.path = tensor;
+    int step = 0;
+    while (step < kThreads / 32 && S.parts[step] > grid) ++step;
+    if (step < kThreads / 32 && length_of(step) - per < afresh) {
+      const int k = (mine + length_of(step) - 1) / length_of(step);
+      int all;
+      const int at = scan<kThreads>(k, S, &all);  // this thread's unit goes to CTAs at ... at + k - 1
+      if (tid < units) {
+        if (blockIdx.x == 0) P.parts[tid] = k > 0 ? make_int2(at, at + k - 1) : make_int2(0, -1);
+        const int j = static_cast<int>(blockIdx.x) - at;
+        if (j >= 0 && j < k) {
+          S.unit = tid;
+          S.unit_start = before;
+          S.first = before + static_cast<int>(static_cast<long long>(mine) * j / k);
+          S.last = before + static_cast<int>(static_cast<long long>(mine) * (j + 1) / k);
+        }
+      }
+      __syncthreads();
+      if (S.unit < units) p.unit = S.unit, p.start = S.unit_start, p.first = S.first, p.last = S.last;
       return p;
     }
   }
@@ -214,7 +217,6 @@ __device__ __forceinline__ Partition cut(const Kv4Params& P, int tensor, int chu
     if (n > 0 && run <= p.first && p.first < run + n) S.unit = u, S.unit_start = run;
     run += n;
   }
-  if (blockIdx.x == 0 && tid == 0) *P.path = tensor;
   __syncthreads();
   p.unit = S.unit;
   p.start = S.unit_start;

@@ -115,7 +115,7 @@ REFUSALS = [
     ("kv4_read", _rows, [("struct_size", 0, SIZE), ("head_dim", 129, UNSUPPORTED), ("v", None, NULL)]),
     ("kv4_verify", _verify, [("struct_size", 0, SIZE), ("batch", -1, RANGE), ("n_q", 0, RANGE), ("n_q_heads", 7, RANGE), ("n_groups", 3, RANGE),
                              ("sm_scale", -1.0, RANGE), ("sm_scale", float("nan"), RANGE), ("tail_len", 65, RANGE), ("tail_len", -1, RANGE),
-                             ("flags", 1, RANGE), ("flags", 6, RANGE), ("head_dim", 64, UNSUPPORTED), ("n_q", 17, UNSUPPORTED), ("n_q", 1 << 30, UNSUPPORTED),
+                             ("flags", 1, RANGE), ("flags", 6, RANGE), ("flags", 4, UNSUPPORTED), ("head_dim", 64, UNSUPPORTED), ("n_q", 17, UNSUPPORTED), ("n_q", 1 << 30, UNSUPPORTED),
                              ("batch", 1025, UNSUPPORTED), ("idx_stride", -1, RANGE), ("idx_stride", (1 << 23) + 1, UNSUPPORTED),
                              ("q", None, NULL), ("kv_len", None, NULL), ("idx", None, NULL), ("counts", None, NULL), ("out", None, NULL),
                              ("lse", None, NULL), ("workspace", None, NULL), ("q", POINTER + 8, ALIGN), ("out", POINTER + 8, ALIGN),
