@@ -618,7 +618,7 @@ int specattn_evict(const specattn_evict_args* args, void* cuda_stream);
  * and KV head of group g (n_groups == 1: all heads; n_groups == n_kv_heads: head g), K and V:
  *   row(dst[b,g,j]) = row(src[b,g,j]).
  * A pool is any array of rows of row_bytes (a multiple of 16) addressed (page, kv, slot, head) by strides
- * in BYTES (multiples of 16; base 16-byte aligned): the bf16 pools of specattn_sparse_verify (256) or
+ * in BYTES (not negative, multiples of 16; base 16-byte aligned): the bf16 pools of specattn_sparse_verify (256) or
  * the codes of a 4-bit cache (64); params, where set, are rows of param_bytes (a multiple of 4) beside
  * them, 4-byte aligned.  No position may be both a source and a destination of a list, nor twice a destination.
  * status (int32 [batch], optional) is cleared by the call and receives SPECATTN_ROW_BAD_INDEX where a

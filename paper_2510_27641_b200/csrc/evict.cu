@@ -17,6 +17,7 @@
 
 #include <atomic>
 
+#include "kv4.cuh"
 #include "nvtx_range.h"
 #include "ptx.cuh"
 #include "specattn.h"
@@ -146,7 +147,7 @@ __global__ void __launch_bounds__(kAccThreads) accumulate_kernel(const __grid_co
 }
 
 // ---- evict ---------------------------------------------------------------------------------------
-constexpr int kEvThreads = 512;
+constexpr int kEvThreads = 1024;
 constexpr int kEvWarps = kEvThreads / 32;
 constexpr int kEvBins = 2048;
 constexpr int kEvMaxCluster = 8;
@@ -160,10 +161,11 @@ struct EvictParams {
   int* positions_out;
   long long L, move_stride;
   int budget, n_sink, n_recent, B, G, slice;
+  int wide;  // whether four neighbouring entries of every array may be read and written at once
 };
 
 struct EvictShared {
-  unsigned hist[3][kEvBins];  // one for each digit: peers may still read the last while a CTA fills the next
+  alignas(8) unsigned hist[3][kEvBins];  // one for each digit: peers may still read the last while a CTA fills the next
   unsigned warp[kEvWarps + 1];
   unsigned found[2];          // digit, keys above it
   unsigned count[3];          // ties, stays behind the budget, gaps in front of it: of this CTA's slice
@@ -210,6 +212,12 @@ __device__ __forceinline__ unsigned ld_peer(const unsigned* local, uint32_t rank
   return v;
 }
 
+__device__ __forceinline__ uint2 ld_peer2(const unsigned* local, uint32_t rank) {
+  uint2 v;
+  asm volatile("ld.shared::cluster.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(map_to_cta(smem_u32(local), rank)) : "memory");
+  return v;
+}
+
 __device__ __forceinline__ uint32_t cluster_size() {
   uint32_t r;
   asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(r));
@@ -250,29 +258,55 @@ __global__ void __launch_bounds__(kEvThreads) evict_kernel(const __grid_constant
   const bool copy_scores = scores_out != nullptr && scores_out != scores;
   const bool copy_positions = positions_out != nullptr && positions_out != positions;
   for (int i = tid; i < 3 * kEvBins; i += kEvThreads) (&S.hist[0][0])[i] = 0;
-  // keys; and copies of what may stay where it is (moves overwrite the rest of it later)
+  __syncthreads();
+  // keys, and the first digit's histogram; copies of what may stay where it is (moves overwrite the rest of it later)
   {
     const long long end = P.seq_len != nullptr ? P.seq_len[b] : n;
     const long long recent = end - P.n_recent;
-    constexpr int kAhead = 8;
-    for (int i0 = tid; i0 < mine; i0 += kAhead * kEvThreads) {
-      float w[kAhead];
-      int pos[kAhead];
+    auto take = [&](int i, float w, int pos) {
+      const uint32_t k = pos < P.n_sink || pos >= recent ? 0xffffffffu : key_of(w);
+      keys[i] = k;
+      atomicAdd(&S.hist[0][k >> 21], 1u);
+    };
+    constexpr int kAhead = 2;  // quads of slots in flight to a thread
+    const bool quads = P.wide && at % 4 == 0;
+    const int whole = quads ? mine & ~3 : 0;
+    for (int i0 = tid * 4; i0 < whole; i0 += kAhead * kEvThreads * 4) {
+      float4 w[kAhead];
+      int4 pos[kAhead];
 #pragma unroll
       for (int j = 0; j < kAhead; ++j) {
-        const int i = i0 + j * kEvThreads;
-        if (i >= mine) continue;
-        w[j] = scores[at + i];
-        pos[j] = positions != nullptr ? positions[at + i] : at + i;
+        const int i = i0 + j * kEvThreads * 4;
+        if (i >= whole) continue;
+        w[j] = *reinterpret_cast<const float4*>(scores + at + i);
+        pos[j] = positions != nullptr ? *reinterpret_cast<const int4*>(positions + at + i) : make_int4(at + i, at + i + 1, at + i + 2, at + i + 3);
       }
 #pragma unroll
       for (int j = 0; j < kAhead; ++j) {
-        const int i = i0 + j * kEvThreads;
-        if (i >= mine) continue;
-        keys[i] = pos[j] < P.n_sink || pos[j] >= recent ? 0xffffffffu : key_of(w[j]);
-        if (copy_scores) scores_out[at + i] = at + i < m ? w[j] : 0.f;
-        if (copy_positions && at + i < m) positions_out[at + i] = pos[j];
+        const int i = i0 + j * kEvThreads * 4;
+        if (i >= whole) continue;
+        take(i, w[j].x, pos[j].x), take(i + 1, w[j].y, pos[j].y), take(i + 2, w[j].z, pos[j].z), take(i + 3, w[j].w, pos[j].w);
+        const int front = m - (at + i);  // of the four, those that lie in front of the budget
+        if (copy_scores)
+          *reinterpret_cast<float4*>(scores_out + at + i) =
+              make_float4(front > 0 ? w[j].x : 0.f, front > 1 ? w[j].y : 0.f, front > 2 ? w[j].z : 0.f, front > 3 ? w[j].w : 0.f);
+        if (copy_positions) {
+          if (front > 3) {
+            *reinterpret_cast<int4*>(positions_out + at + i) = pos[j];
+          } else {
+            if (front > 0) positions_out[at + i] = pos[j].x;
+            if (front > 1) positions_out[at + i + 1] = pos[j].y;
+            if (front > 2) positions_out[at + i + 2] = pos[j].z;
+          }
+        }
       }
+    }
+    for (int i = whole + tid; i < mine; i += kEvThreads) {
+      const float w = scores[at + i];
+      const int pos = positions != nullptr ? positions[at + i] : at + i;
+      take(i, w, pos);
+      if (copy_scores) scores_out[at + i] = at + i < m ? w : 0.f;
+      if (copy_positions && at + i < m) positions_out[at + i] = pos;
     }
   }
   if (n == m) {  // everything stays (the same for the whole cluster)
@@ -289,23 +323,25 @@ __global__ void __launch_bounds__(kEvThreads) evict_kernel(const __grid_constant
     const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
     const uint32_t digit_mask = (1u << bits) - 1u, above = pass == 0 ? 0u : ~((1u << (shift + bits)) - 1u);
     unsigned* hist = S.hist[pass];
-    for (int i = tid; i < mine; i += kEvThreads) {
-      const uint32_t k = keys[i];
-      if ((k & above) == prefix) atomicAdd(&hist[(k >> shift) & digit_mask], 1u);
+    if (pass > 0) {
+      for (int i = tid; i < mine; i += kEvThreads) {
+        const uint32_t k = keys[i];
+        if ((k & above) == prefix) atomicAdd(&hist[(k >> shift) & digit_mask], 1u);
+      }
     }
     cluster_sync();
-    // every CTA adds up all histograms; a thread has four neighbouring bins, the largest digits first
-    const int top = kEvBins - 4 - 4 * tid;
-    unsigned c[4] = {0, 0, 0, 0};
+    // every CTA adds up all histograms; a thread has two neighbouring bins, the largest digits first
+    const int top = kEvBins - 2 - 2 * tid;
+    unsigned c[2] = {0, 0};
     for (uint32_t r = 0; r < n_cta; ++r) {
-      const float4 v = ld_cluster_v4(map_to_cta(smem_u32(&hist[top]), r));
-      c[0] += __float_as_uint(v.x), c[1] += __float_as_uint(v.y), c[2] += __float_as_uint(v.z), c[3] += __float_as_uint(v.w);
+      const uint2 v = ld_peer2(&hist[top], r);
+      c[0] += v.x, c[1] += v.y;
     }
     unsigned total;
-    const unsigned before = block_prefix(c[0] + c[1] + c[2] + c[3], S.warp, &total);
+    const unsigned before = block_prefix(c[0] + c[1], S.warp, &total);
     unsigned run = before;
 #pragma unroll
-    for (int e = 3; e >= 0; --e) {
+    for (int e = 1; e >= 0; --e) {
       if (run < want && run + c[e] >= want) {
         S.found[0] = static_cast<unsigned>(top + e);
         S.found[1] = run;
@@ -420,88 +456,90 @@ struct MoveParams {
   int* status;
   long long table_stride, move_stride;
   int B, G, heads, page_size, units, words, per_block;  // units: 16-byte pieces of a row; words: 4-byte pieces of its params
+  FastDiv by_page, by_heads, by_units, by_words;
 };
 
-__device__ __forceinline__ bool place_of(const MoveParams& P, int b, int pos, int* page, int* slot) {
-  if (pos < 0) return false;
-  const int pi = pos / P.page_size;
-  if (pi >= P.table_stride) return false;
-  const long long at = static_cast<long long>(b) * P.table_stride + pi;
-  const long long p = P.table != nullptr ? static_cast<long long>(P.table[at]) : at;
-  if (p < 0 || p >= P.n_pages) return false;
-  *page = static_cast<int>(p);
-  *slot = pos - pi * P.page_size;
-  return true;
+// Where the row of a position begins in an array of the given strides, or -1.
+struct Place {
+  int page, slot;
+};
+__device__ __forceinline__ Place place_of(const MoveParams& P, int b, int pos) {
+  Place p = {-1, 0};
+  if (pos < 0) return p;
+  const int pi = pos / P.by_page;
+  p.page = static_cast<int>(page_of(P.table, P.table_stride, P.n_pages, b, pi));
+  p.slot = pos - pi * P.page_size;
+  return p;
 }
 
 // A block carries out up to per_block moves of one list in one pool: it looks up where their rows lie, then copies
-// them in pieces of 16 bytes, four in flight to a thread.
+// them in pieces of 16 bytes, four in flight to a thread, and their params in words.
 __global__ void __launch_bounds__(kMoveThreads) move_rows_kernel(const __grid_constant__ MoveParams P) {
-  __shared__ int4 place[kMoveMost];  // page and slot of source and destination; page -1: not to be moved
+  __shared__ longlong2 row[kMoveMost], word[kMoveMost];  // offsets of source and destination; source -1: not to be moved
   const int b = blockIdx.y / P.G, g = blockIdx.y - b * P.G;
   const long long j0 = static_cast<long long>(blockIdx.x) * P.per_block;
   const int n = static_cast<int>(min(static_cast<long long>(P.per_block), min(static_cast<long long>(P.n_moves[blockIdx.y]), P.move_stride) - j0));
   if (n <= 0) return;
   const long long first = static_cast<long long>(blockIdx.y) * P.move_stride + j0;
+  const int group = P.G > 1 ? g : 0;
   for (int j = threadIdx.x; j < n; j += kMoveThreads) {
-    int4 p;
-    const bool ok = place_of(P, b, P.src[first + j], &p.x, &p.y) & place_of(P, b, P.dst[first + j], &p.z, &p.w);
-    if (!ok) {
-      p.x = -1;
+    const Place from = place_of(P, b, P.src[first + j]), into = place_of(P, b, P.dst[first + j]);
+    if (from.page < 0 || into.page < 0) {
+      row[j] = word[j] = make_longlong2(-1, -1);
       if (P.status != nullptr) atomicOr(P.status + b, SPECATTN_ROW_BAD_INDEX);
+      continue;
     }
-    place[j] = p;
+    row[j] = make_longlong2(from.page * P.s_page + from.slot * P.s_slot + group * P.s_head, into.page * P.s_page + into.slot * P.s_slot + group * P.s_head);
+    word[j] = make_longlong2(from.page * P.p_page + from.slot * P.p_slot + group * P.p_head, into.page * P.p_page + into.slot * P.p_slot + group * P.p_head);
   }
   __syncthreads();
   const int heads = P.G > 1 ? 1 : P.heads;  // of a group
-  unsigned char* pool = P.pool[blockIdx.z];
-  const int total = n * 2 * heads * P.units;
-  auto piece = [&](int x, int units, int width, long long s_page, long long s_kv, long long s_slot, long long s_head,
-                   long long* from, long long* into) {
-    int rest = x / units;
-    const int u = x - rest * units;
-    int up = rest / heads;
-    const int h = rest - up * heads + (P.G > 1 ? g : 0);
-    const int4 p = place[up >> 1];
-    if (p.x < 0) return false;
-    const long long same = (up & 1) * s_kv + h * s_head + static_cast<long long>(u) * width;
-    *from = p.x * s_page + p.y * s_slot + same;
-    *into = p.z * s_page + p.w * s_slot + same;
-    return true;
-  };
+  const FastDiv by_heads = P.by_heads;      // (by 1 where that is so)
   constexpr int kAhead = 4;
-  for (int x0 = threadIdx.x; x0 < total; x0 += kMoveThreads * kAhead) {
-    uint4 v[kAhead];
-    long long into[kAhead];
-    bool ok[kAhead];
+  {
+    unsigned char* const pool = P.pool[blockIdx.z];
+    const int total = n * 2 * heads * P.units;
+    for (int x0 = threadIdx.x; x0 < total; x0 += kMoveThreads * kAhead) {
+      uint4 v[kAhead];
+      unsigned char* into[kAhead];
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
-      const int x = x0 + k * kMoveThreads;
-      long long from;
-      ok[k] = x < total && piece(x, P.units, 16, P.s_page, P.s_kv, P.s_slot, P.s_head, &from, &into[k]);
-      if (ok[k]) v[k] = __ldcs(reinterpret_cast<const uint4*>(pool + from));
+      for (int k = 0; k < kAhead; ++k) {
+        const int x = x0 + k * kMoveThreads;
+        into[k] = nullptr;
+        if (x >= total) continue;
+        const int rest = x / P.by_units, up = rest / by_heads, h = rest - up * heads;
+        const longlong2 at = row[up >> 1];
+        if (at.x < 0) continue;
+        const long long same = (up & 1 ? P.s_kv : 0) + h * P.s_head + (x - rest * P.units) * 16;
+        into[k] = pool + at.y + same;
+        v[k] = __ldcs(reinterpret_cast<const uint4*>(pool + at.x + same));
+      }
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k)
+        if (into[k] != nullptr) __stcs(reinterpret_cast<uint4*>(into[k]), v[k]);
     }
-#pragma unroll
-    for (int k = 0; k < kAhead; ++k)
-      if (ok[k]) __stcs(reinterpret_cast<uint4*>(pool + into[k]), v[k]);
   }
   if (P.words == 0) return;
-  unsigned char* param = P.param[blockIdx.z];
-  const int total_words = n * 2 * heads * P.words;
-  for (int x0 = threadIdx.x; x0 < total_words; x0 += kMoveThreads * kAhead) {
+  unsigned char* const param = P.param[blockIdx.z];
+  const int total = n * 2 * heads * P.words;
+  for (int x0 = threadIdx.x; x0 < total; x0 += kMoveThreads * kAhead) {
     uint32_t v[kAhead];
-    long long into[kAhead];
-    bool ok[kAhead];
+    unsigned char* into[kAhead];
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
       const int x = x0 + k * kMoveThreads;
-      long long from;
-      ok[k] = x < total_words && piece(x, P.words, 4, P.p_page, P.p_kv, P.p_slot, P.p_head, &from, &into[k]);
-      if (ok[k]) v[k] = *reinterpret_cast<const uint32_t*>(param + from);
+      into[k] = nullptr;
+      if (x >= total) continue;
+      const int rest = x / P.by_words, up = rest / by_heads, h = rest - up * heads;
+      const longlong2 at = word[up >> 1];
+      if (at.x < 0) continue;
+      const long long same = (up & 1 ? P.p_kv : 0) + h * P.p_head + (x - rest * P.words) * 4;
+      into[k] = param + at.y + same;
+      v[k] = *reinterpret_cast<const uint32_t*>(param + at.x + same);
     }
 #pragma unroll
     for (int k = 0; k < kAhead; ++k)
-      if (ok[k]) *reinterpret_cast<uint32_t*>(param + into[k]) = v[k];
+      if (into[k] != nullptr) *reinterpret_cast<uint32_t*>(into[k]) = v[k];
   }
 }
 
@@ -630,7 +668,9 @@ extern "C" int specattn_evict(const specattn_evict_args* args, void* cuda_stream
   // a CTA to 8192 slots, up to eight; no more than the slots need while there are lists enough for all SMs
   int ctas = 1;
   while (ctas < kEvMaxCluster && ctas * 8192 < A.L && (lists * ctas < 296 || ctas * kEvMaxSlice < A.L)) ctas *= 2;
-  P.slice = static_cast<int>((A.L + ctas - 1) / ctas);
+  P.slice = static_cast<int>(((A.L + ctas - 1) / ctas + 3) / 4 * 4);
+  P.wide = A.L % 4 == 0 && ((reinterpret_cast<uintptr_t>(A.scores) | reinterpret_cast<uintptr_t>(A.positions) |
+                             reinterpret_cast<uintptr_t>(A.scores_out) | reinterpret_cast<uintptr_t>(A.positions_out)) % 16 == 0);
   const size_t smem = static_cast<size_t>(P.slice) * sizeof(uint32_t);
   static std::atomic<unsigned long long> prepared{0};  // a bit per device
   int dev = 0;
@@ -672,7 +712,8 @@ extern "C" int specattn_move_rows(const specattn_move_args* args, void* cuda_str
   if (args == nullptr) return SPECATTN_ERR_NULL;
   if (args->struct_size != sizeof(specattn_move_args)) return SPECATTN_ERR_STRUCT_SIZE;
   const specattn_move_args& A = *args;
-  if (A.n_pools < 0 || A.batch < 0 || A.n_kv_heads < 1 || A.page_size < 1 || A.n_pages < 1 || A.n_pages > INT32_MAX ||
+  if (A.stride_page < 0 || A.stride_kv < 0 || A.stride_slot < 0 || A.stride_head < 0 || A.pstride_page < 0 || A.pstride_kv < 0 ||
+      A.pstride_slot < 0 || A.pstride_head < 0 || A.n_pools < 0 || A.batch < 0 || A.n_kv_heads < 1 || A.page_size < 1 || A.n_pages < 1 || A.n_pages > INT32_MAX ||
       (A.n_groups != 1 && A.n_groups != A.n_kv_heads) || A.block_table_stride < 0 || A.move_stride < 0 || A.row_bytes < 16 ||
       A.row_bytes > 4096 || A.param_bytes < 0 || A.param_bytes > 256)
     return SPECATTN_ERR_RANGE;
@@ -715,6 +756,10 @@ extern "C" int specattn_move_rows(const specattn_move_args* args, void* cuda_str
   P.page_size = A.page_size;
   P.units = static_cast<int>(A.row_bytes / 16);
   P.words = static_cast<int>(A.param_bytes / 4);
+  P.by_page = fast_div(A.page_size);
+  P.by_heads = fast_div(A.n_groups > 1 ? 1 : A.n_kv_heads);
+  P.by_units = fast_div(P.units);
+  P.by_words = fast_div(P.words > 0 ? P.words : 1);
   // about 64 KB to a block: long enough to hide the lookups, short enough to spread a few moves
   const long long bytes = 2 * A.row_bytes * (A.n_groups > 1 ? 1 : A.n_kv_heads);
   long long per = 65536 / bytes;
