@@ -5,7 +5,7 @@
 //               (head, query) in binary64 (a conversion and an addition a value: 1/8 of the SM's binary64 rate at
 //               HBM's speed).  Few positions are dealt to several threads each, by rows.
 //   evict       one list to a cluster of CTAs that hold its weights as ordered 32-bit keys in shared memory.  The
-//               m-th largest key is found digit by digit (11 + 11 + 10 bits) from histograms that the cluster adds
+//               m-th largest key is found digit by digit (four of 8 bits) from histograms that the cluster adds
 //               up; which slots stay then follows from comparisons, and their ranks from counts.  Bound by the
 //               chain of passes and cluster barriers.
 //   move_rows   copies of rows, bound by HBM.
@@ -147,9 +147,8 @@ __global__ void __launch_bounds__(kAccThreads) accumulate_kernel(const __grid_co
 }
 
 // ---- evict ---------------------------------------------------------------------------------------
-constexpr int kEvThreads = 1024;
-constexpr int kEvWarps = kEvThreads / 32;
-constexpr int kEvBins = 2048;
+constexpr int kEvBins = 256;
+constexpr int kEvCopies = 8;  // of a histogram: weights share their leading bits, and lanes that meet in a bin wait for one another
 constexpr int kEvMaxCluster = 8;
 constexpr int kEvMaxSlice = SPECATTN_MAX_KV_LEN / kEvMaxCluster;  // keys of a CTA
 
@@ -165,10 +164,11 @@ struct EvictParams {
 };
 
 struct EvictShared {
-  alignas(8) unsigned hist[3][kEvBins];  // one for each digit: peers may still read the last while a CTA fills the next
-  unsigned warp[kEvWarps + 1];
-  unsigned found[2];          // digit, keys above it
-  unsigned count[3];          // ties, stays behind the budget, gaps in front of it: of this CTA's slice
+  alignas(16) unsigned hist[4][kEvBins * kEvCopies];  // one for each digit; copy c of bin d at d * kEvCopies + c
+  unsigned sums[4][kEvBins];                          // of the copies, for the peers
+  unsigned warp[33];
+  unsigned found[3];  // digit, keys above it, keys at it
+  unsigned count[2];  // of this CTA's slice: ties; stays behind the budget, and from bit 16 on gaps in front of it
 };
 
 // Larger weight, larger key; every key of a slot that exists is above 0, a protected slot's above all weights'.
@@ -180,6 +180,7 @@ __device__ __forceinline__ uint32_t key_of(float w) {
 }
 
 // The exclusive prefix of v over the threads of the CTA and its total.
+template <int kThreads>
 __device__ __forceinline__ unsigned block_prefix(unsigned v, unsigned* warp_sums, unsigned* total) {
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
   unsigned x = v;
@@ -191,30 +192,21 @@ __device__ __forceinline__ unsigned block_prefix(unsigned v, unsigned* warp_sums
   __syncthreads();  // the last call's sums have been read
   if (lane == 31) warp_sums[w] = x;
   __syncthreads();
-  if (w == 0) {
-    unsigned s = lane < kEvWarps ? warp_sums[lane] : 0, t = s;
+  // (every warp adds up the others' for itself)
+  unsigned t = lane < kThreads / 32 ? warp_sums[lane] : 0u;
+  const unsigned mine = t;
 #pragma unroll
-    for (int o = 1; o < kEvWarps; o <<= 1) {
-      const unsigned y = __shfl_up_sync(0xffffffffu, t, o);
-      if (lane >= o) t += y;
-    }
-    if (lane < kEvWarps) warp_sums[lane] = t - s;
-    if (lane == kEvWarps - 1) warp_sums[kEvWarps] = t;
+  for (int o = 1; o < 32; o <<= 1) {
+    const unsigned y = __shfl_up_sync(0xffffffffu, t, o);
+    if (lane >= o) t += y;
   }
-  __syncthreads();
-  *total = warp_sums[kEvWarps];
-  return warp_sums[w] + x - v;
+  *total = __shfl_sync(0xffffffffu, t, 31);
+  return __shfl_sync(0xffffffffu, t - mine, w) + x - v;
 }
 
 __device__ __forceinline__ unsigned ld_peer(const unsigned* local, uint32_t rank) {
   unsigned v;
   asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(map_to_cta(smem_u32(local), rank)) : "memory");
-  return v;
-}
-
-__device__ __forceinline__ uint2 ld_peer2(const unsigned* local, uint32_t rank) {
-  uint2 v;
-  asm volatile("ld.shared::cluster.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(map_to_cta(smem_u32(local), rank)) : "memory");
   return v;
 }
 
@@ -229,17 +221,12 @@ __device__ __forceinline__ void cluster_sync() {
   cluster_wait();
 }
 
-// Sum of count[which] over the CTAs of the cluster in front of this one.
-__device__ __forceinline__ unsigned peers_before(const EvictShared& S, int which, uint32_t rank) {
-  unsigned sum = 0;
-  for (uint32_t r = 0; r < rank; ++r) sum += ld_peer(&S.count[which], r);
-  return sum;
-}
-
 // One list to a cluster.  Slots are dealt to the CTAs in slices and, within a slice, to warps in runs of 32, so that
 // ranks in slot order are sums over runs: a thread that owns a run's lane learns its rank from the ballot, the runs in
 // front of it in its warp's stretch, and the stretches in front of that.
+template <int kEvThreads>
 __global__ void __launch_bounds__(kEvThreads) evict_kernel(const __grid_constant__ EvictParams P) {
+  constexpr int kEvWarps = kEvThreads / 32;
   extern __shared__ uint32_t keys[];
   __shared__ EvictShared S;
   const uint32_t rank = cluster_cta_rank(), n_cta = cluster_size();
@@ -257,7 +244,7 @@ __global__ void __launch_bounds__(kEvThreads) evict_kernel(const __grid_constant
   const int mine = max(0, min(P.slice, n - at));
   const bool copy_scores = scores_out != nullptr && scores_out != scores;
   const bool copy_positions = positions_out != nullptr && positions_out != positions;
-  for (int i = tid; i < 3 * kEvBins; i += kEvThreads) (&S.hist[0][0])[i] = 0;
+  for (int i = tid; i < kEvBins * kEvCopies; i += kEvThreads) reinterpret_cast<uint4*>(&S.hist[0][0])[i] = make_uint4(0u, 0u, 0u, 0u);
   __syncthreads();
   // keys, and the first digit's histogram; copies of what may stay where it is (moves overwrite the rest of it later)
   {
@@ -266,7 +253,7 @@ __global__ void __launch_bounds__(kEvThreads) evict_kernel(const __grid_constant
     auto take = [&](int i, float w, int pos) {
       const uint32_t k = pos < P.n_sink || pos >= recent ? 0xffffffffu : key_of(w);
       keys[i] = k;
-      atomicAdd(&S.hist[0][k >> 21], 1u);
+      atomicAdd(&S.hist[0][(k >> 24) * kEvCopies + (lane & (kEvCopies - 1))], 1u);
     };
     constexpr int kAhead = 2;  // quads of slots in flight to a thread
     const bool quads = P.wide && at % 4 == 0;
@@ -316,44 +303,38 @@ __global__ void __launch_bounds__(kEvThreads) evict_kernel(const __grid_constant
   __syncthreads();
 
   // the m-th largest key: its digits, and how many of the keys equal to it stay
-  uint32_t prefix = 0;   // the digits found so far
+  uint32_t prefix = 0;  // the digits found so far
   unsigned want = static_cast<unsigned>(m), ties = 0;
 #pragma unroll 1
-  for (int pass = 0; pass < 3; ++pass) {
-    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
-    const uint32_t digit_mask = (1u << bits) - 1u, above = pass == 0 ? 0u : ~((1u << (shift + bits)) - 1u);
-    unsigned* hist = S.hist[pass];
+  for (int pass = 0; pass < 4; ++pass) {
+    const int shift = 24 - 8 * pass;
     if (pass > 0) {
+      const uint32_t above = 0xffffff00u << shift;
+      unsigned* hist = S.hist[pass] + (lane & (kEvCopies - 1));
+#pragma unroll 4
       for (int i = tid; i < mine; i += kEvThreads) {
         const uint32_t k = keys[i];
-        if ((k & above) == prefix) atomicAdd(&hist[(k >> shift) & digit_mask], 1u);
+        if ((k & above) == prefix) atomicAdd(&hist[((k >> shift) & 255u) * kEvCopies], 1u);
       }
+      __syncthreads();
+    }
+    if (tid < kEvBins) {
+      const uint4 a = *reinterpret_cast<const uint4*>(&S.hist[pass][tid * kEvCopies]), b4 = *reinterpret_cast<const uint4*>(&S.hist[pass][tid * kEvCopies + 4]);
+      S.sums[pass][tid] = (a.x + a.y + a.z + a.w) + (b4.x + b4.y + b4.z + b4.w);
     }
     cluster_sync();
-    // every CTA adds up all histograms; a thread has two neighbouring bins, the largest digits first
-    const int top = kEvBins - 2 - 2 * tid;
-    unsigned c[2] = {0, 0};
-    for (uint32_t r = 0; r < n_cta; ++r) {
-      const uint2 v = ld_peer2(&hist[top], r);
-      c[0] += v.x, c[1] += v.y;
-    }
+    // every CTA adds up all histograms, the largest digits first
+    const int digit = kEvBins - 1 - tid;
+    unsigned c = 0;
+    if (tid < kEvBins)
+      for (uint32_t r = 0; r < n_cta; ++r) c += ld_peer(&S.sums[pass][digit], r);
     unsigned total;
-    const unsigned before = block_prefix(c[0] + c[1], S.warp, &total);
-    unsigned run = before;
-#pragma unroll
-    for (int e = 1; e >= 0; --e) {
-      if (run < want && run + c[e] >= want) {
-        S.found[0] = static_cast<unsigned>(top + e);
-        S.found[1] = run;
-        S.count[0] = c[e];
-      }
-      run += c[e];
-    }
+    const unsigned run = block_prefix<kEvThreads>(c, S.warp, &total);
+    if (run < want && run + c >= want) S.found[0] = static_cast<unsigned>(digit), S.found[1] = run, S.found[2] = c;
     __syncthreads();
     prefix |= S.found[0] << shift;
     want -= S.found[1];
-    ties = S.count[0];
-    __syncthreads();
+    ties = S.found[2];
   }
   const uint32_t cut = prefix;  // slots above it stay, and the first `want` of the `ties` slots at it
 
@@ -366,10 +347,11 @@ __global__ void __launch_bounds__(kEvThreads) evict_kernel(const __grid_constant
     unsigned t = 0;
     for (int i = w0 + lane; i < w1; i += 32) t += keys[i] == cut ? 1u : 0u;
     unsigned total;
-    const unsigned before = block_prefix(t, S.warp, &total);
+    const unsigned before = block_prefix<kEvThreads>(t, S.warp, &total);
     if (tid == 0) S.count[0] = total;
     cluster_sync();
-    tie_rank = __shfl_sync(0xffffffffu, before, 0) + peers_before(S, 0, rank);
+    tie_rank = __shfl_sync(0xffffffffu, before, 0);
+    for (uint32_t r = 0; r < rank; ++r) tie_rank += ld_peer(&S.count[0], r);
   }
   auto ballots = [&](int i, unsigned* ties_so_far) {  // which of the 32 slots from i on stay
     const uint32_t k = i + lane < w1 ? keys[i + lane] : 0u;
@@ -382,6 +364,7 @@ __global__ void __launch_bounds__(kEvThreads) evict_kernel(const __grid_constant
     return __ballot_sync(0xffffffffu, stays && i + lane < w1);
   };
   unsigned n_from = 0, n_into = 0, seen = tie_rank;
+#pragma unroll 4
   for (int i = w0; i < w1; i += 32) {
     const unsigned stays = ballots(i, &seen);
     const unsigned exist = w1 - i >= 32 ? 0xffffffffu : (1u << (w1 - i)) - 1u;
@@ -390,19 +373,26 @@ __global__ void __launch_bounds__(kEvThreads) evict_kernel(const __grid_constant
     n_from += __popc(stays & ~in_front);
     n_into += __popc(exist & ~stays & in_front);
   }
-  unsigned total_from, total_into;
-  const unsigned from0 = block_prefix(lane == 0 ? n_from : 0u, S.warp, &total_from);
-  const unsigned into0 = block_prefix(lane == 0 ? n_into : 0u, S.warp, &total_into);
-  if (tid == 0) S.count[1] = total_from, S.count[2] = total_into;
+  // (a slice has fewer than 2^16 slots: both counts in one word)
+  unsigned total_both;
+  const unsigned both = block_prefix<kEvThreads>(lane == 0 ? n_from | n_into << 16 : 0u, S.warp, &total_both);
+  if (tid == 0) S.count[1] = total_both;
   cluster_sync();
-  unsigned from = __shfl_sync(0xffffffffu, from0, 0) + peers_before(S, 1, rank);
-  unsigned into = __shfl_sync(0xffffffffu, into0, 0) + peers_before(S, 2, rank);
-  if (rank == n_cta - 1 && tid == 0) P.n_moves[list] = static_cast<int>(peers_before(S, 1, rank) + total_from);
+  unsigned from = __shfl_sync(0xffffffffu, both, 0), into = from >> 16;
+  from &= 0xffffu;
+  for (uint32_t r = 0; r < rank; ++r) {
+    const unsigned x = ld_peer(&S.count[1], r);
+    from += x & 0xffffu;
+    into += x >> 16;
+  }
+  // (the last thread's count is where the last slice ends)
+  if (rank == n_cta - 1 && tid == kEvThreads - 1) P.n_moves[list] = static_cast<int>(from + n_from);
 
   // the lists, and what stays where it is
   int* src = P.src + list * P.move_stride;
   int* dst = P.dst + list * P.move_stride;
   seen = tie_rank;
+#pragma unroll 4
   for (int i = w0; i < w1; i += 32) {
     const unsigned stays = ballots(i, &seen);
     const unsigned exist = w1 - i >= 32 ? 0xffffffffu : (1u << (w1 - i)) - 1u;
@@ -672,23 +662,26 @@ extern "C" int specattn_evict(const specattn_evict_args* args, void* cuda_stream
   P.wide = A.L % 4 == 0 && ((reinterpret_cast<uintptr_t>(A.scores) | reinterpret_cast<uintptr_t>(A.positions) |
                              reinterpret_cast<uintptr_t>(A.scores_out) | reinterpret_cast<uintptr_t>(A.positions_out)) % 16 == 0);
   const size_t smem = static_cast<size_t>(P.slice) * sizeof(uint32_t);
-  static std::atomic<unsigned long long> prepared{0};  // a bit per device
+  // 1024 threads where a CTA has an SM to itself: 8 lists of 32768 18 against 20 us; of 512 two fit, and 256 CTAs run at once
+  const bool many = lists * ctas > device_sm_count();
+  const auto kernel = many ? evict_kernel<512> : evict_kernel<1024>;
+  static std::atomic<unsigned long long> prepared[2];  // a bit per device
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) {
     cudaGetLastError();
     return SPECATTN_ERR_CUDA;
   }
-  if (!((prepared.load(std::memory_order_acquire) >> dev) & 1ull)) {
-    if (cudaFuncSetAttribute(evict_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kEvMaxSlice * 4) != cudaSuccess) {
+  if (!((prepared[many].load(std::memory_order_acquire) >> dev) & 1ull)) {
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kEvMaxSlice * 4) != cudaSuccess) {
       cudaGetLastError();
       return SPECATTN_ERR_CUDA;
     }
-    prepared.fetch_or(1ull << dev, std::memory_order_release);
+    prepared[many].fetch_or(1ull << dev, std::memory_order_release);
   }
   cudaLaunchConfig_t cfg;
   memset(&cfg, 0, sizeof(cfg));
   cfg.gridDim = dim3(static_cast<unsigned>(lists * ctas));
-  cfg.blockDim = dim3(kEvThreads);
+  cfg.blockDim = dim3(many ? 512 : 1024);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = static_cast<cudaStream_t>(cuda_stream);
   cudaLaunchAttribute attr[1];
@@ -698,7 +691,7 @@ extern "C" int specattn_evict(const specattn_evict_args* args, void* cuda_stream
   attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  if (cudaLaunchKernelEx(&cfg, evict_kernel, P) != cudaSuccess) {
+  if (cudaLaunchKernelEx(&cfg, kernel, P) != cudaSuccess) {
     cudaGetLastError();
     return SPECATTN_ERR_CUDA;
   }
