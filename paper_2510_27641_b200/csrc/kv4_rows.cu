@@ -83,24 +83,24 @@ template <bool kHalf>
 __device__ __forceinline__ uint32_t encode(const uint4& x, float lo, float inv) {
   if (inv == 0.f) return 0;  // (a constant row, or none of finite span)
   const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-  float d[8], c[8], far = kHalf && inv > 16384.f ? 1.f : 0.f;
+  float c[8], far = kHalf && inv > 16384.f ? 1.f : 0.f;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const float2 p = widen<kHalf>(w[i]);
-    d[2 * i] = __fsub_rn(p.x, lo);
-    d[2 * i + 1] = __fsub_rn(p.y, lo);
-  }
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float q = __fmul_rn(d[i], inv);
-    c[i] = __fsub_rn(__fadd_rn(q, kRound), kRound);
-    far = fmaxf(far, fabsf(__fsub_rn(q, c[i])));
+    const Two q = mul2(add2(two(p.x, p.y), two(-lo, -lo)), two(inv, inv));
+    const Two r = add2(add2(q, two(kRound, kRound)), two(-kRound, -kRound));
+    const float2 off = each(fma2(r, two(-1.f, -1.f), q)), code = each(r);
+    c[2 * i] = code.x, c[2 * i + 1] = code.y;
+    far = fmaxf(far, fmaxf(fabsf(off.x), fabsf(off.y)));
   }
   if (far > 0.49999f) {
     // the scale, which is a 16-bit value, back from its rounded inverse
     const float s = widen<kHalf>(narrow<kHalf>(__fdiv_rn(1.f, inv), 0.f)).x;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) c[i] = fminf(rintf(__fdiv_rn(d[i], s)), 15.f);
+    for (int i = 0; i < 8; ++i) {
+      const float2 p = widen<kHalf>(w[i >> 1]);
+      c[i] = fminf(rintf(__fdiv_rn(__fsub_rn(i & 1 ? p.y : p.x, lo), s)), 15.f);
+    }
   }
   // four codes are a number below 2^16, exact in binary32
   const float a = fmaf(fmaf(c[3], 16.f, c[2]), 256.f, fmaf(c[1], 16.f, c[0]));
@@ -192,14 +192,16 @@ __global__ void __launch_bounds__(kThreads, 4) kv4_rows_kernel(const __grid_cons
       for (int j = 0; j < kRows; ++j) {
         const unsigned long long into = __shfl_sync(mask, code_at >= 0 ? reinterpret_cast<unsigned long long>(at) : 0ull, j, 16);
         const float2 p = widen<kHalf>(__shfl_sync(mask, sz, j, 16));
+        const uint32_t low = c[j] & 0x0f0f0f0fu, high = (c[j] >> 4) & 0x0f0f0f0fu;
         uint32_t w[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          // (a code in the low bits of 2^23 is that number; a product of 11 by 4 bits is exact, so the fused form rounds
-          // once like the separate one)
-          const float lo = __uint_as_float(((c[j] >> (8 * i)) & 15u) | 0x4b000000u) - 8388608.f;
-          const float hi = __uint_as_float(((c[j] >> (8 * i + 4)) & 15u) | 0x4b000000u) - 8388608.f;
-          w[i] = narrow<kHalf>(fmaf(p.x, lo, p.y), fmaf(p.x, hi, p.y));
+          // (a code in the lowest byte of 2^23 makes 2^23 and that number; a product of 11 by 4 bits is exact, so the fused
+          // form rounds once like the separate one)
+          const float a = __uint_as_float(__byte_perm(low, 0x4b000000u, 0x7650 + i)),
+                      b = __uint_as_float(__byte_perm(high, 0x4b000000u, 0x7650 + i));
+          const float2 x = each(fma2(two(p.x, p.x), add2(two(a, b), two(-8388608.f, -8388608.f)), two(p.y, p.y)));
+          w[i] = narrow<kHalf>(x.x, x.y);
         }
         if (into != 0) __stcs(reinterpret_cast<uint4*>(into + lane * 16), make_uint4(w[0], w[1], w[2], w[3]));
       }
