@@ -459,7 +459,8 @@ typedef struct specattn_kv4_cache {
  * aligned, strides multiples of 8.  n_new == NULL: n_tokens of every sequence (values beyond
  * [0, n_tokens] are clamped).  status (int32 [batch], optional) is cleared by the call and receives
  * SPECATTN_ROW_BAD_INDEX where a position is negative or beyond the block table or its page id out of range
- * (that row is skipped) and, on append, SPECATTN_ROW_INVALID_VALUE.  head_dim == 128. */
+ * (that row is skipped) and, on append, SPECATTN_ROW_INVALID_VALUE.  No two rows of a call may be written to one
+ * place (a page in two sequences' tables, overlapping k or v of a read).  head_dim == 128. */
 typedef struct specattn_kv4_rows_args {
   uint32_t struct_size;
   int32_t batch;
@@ -496,12 +497,19 @@ int specattn_kv4_read(const specattn_kv4_rows_args* args, void* cuda_stream);
  * position is outside [0, kv_len[b]), a position beyond the block table or its page id out of range
  * (such entries are read from position 0 / page 0 instead), else 0.
  * Positions whose row holds NaN make the rows that attend them NaN; rows that no list names, masked tail rows
- * and the rest of the last page are not looked at.
+ * and the rest of the last page are not looked at.  Values are summed before the division by sum p_i: their magnitude
+ * times the number of positions has to stay within binary32.  A weight's product with its row's scale keeps its 11 bits while
+ * it is at least 2^-19 of the largest scale of the rows that the query has met.
+ * out must not overlap q.
  * Requirements: head_dim == 128; n_q * (n_q_heads / n_kv_heads) <= 64; batch * n_kv_heads <= 2048; lists
- * and, where dense, block_table_stride * page_size of at most 2^23 positions.
+ * and, where dense, block_table_stride * page_size of at most 2^23 positions; and (SPECATTN_ERR_UNSUPPORTED otherwise)
+ * no negative stride, the codes of one head within 64 GB and its params within 16 GB of their first
+ * (n_pages * stride_page + stride_kv + page_size * stride_slot).
  * flags: SPECATTN_VERIFY_ENGINE_MMA_SYNC or SPECATTN_VERIFY_ENGINE_TCGEN05 forces one of two implementations of the same
- * operation; TCGEN05 runs 17 to 48 query rows (SPECATTN_ERR_UNSUPPORTED otherwise).  With neither the kernel itself picks, by
- * the rows and by the lengths that it finds.  Results agree within the tolerance of the operation either way.
+ * operation; TCGEN05 runs 33 to 40 query rows (SPECATTN_ERR_UNSUPPORTED otherwise).  With neither the library picks by the
+ * sizes of the call: a caller of 33 to 40 rows whose lists are far shorter than idx_stride or the block
+ * table (fewer than 1024 positions an SM in all) does better to force MMA_SYNC.  Results agree within the tolerance of the
+ * operation either way.
  * workspace: specattn_kv4_verify_workspace_bytes() bytes, 256-byte aligned, no preparation and no
  * state between calls; two calls that may overlap on the GPU need separate ones.
  * (The call signals programmatic launch completion early: it does not count as the launch in front of a
@@ -620,7 +628,8 @@ int specattn_evict(const specattn_evict_args* args, void* cuda_stream);
  * A pool is any array of rows of row_bytes (a multiple of 16) addressed (page, kv, slot, head) by strides
  * in BYTES (not negative, multiples of 16; base 16-byte aligned): the bf16 pools of specattn_sparse_verify (256) or
  * the codes of a 4-bit cache (64); params, where set, are rows of param_bytes (a multiple of 4) beside
- * them, 4-byte aligned.  No position may be both a source and a destination of a list, nor twice a destination.
+ * them, 4-byte aligned.  No position may be both a source and a destination of a list, nor twice a destination; and no
+ * page that a move reads or writes may be in two sequences' tables (a shared prefix has to be copied first).
  * status (int32 [batch], optional) is cleared by the call and receives SPECATTN_ROW_BAD_INDEX where a
  * position is negative or beyond the block table, or its page id outside [0, n_pages) (the move is skipped). */
 typedef struct specattn_move_args {

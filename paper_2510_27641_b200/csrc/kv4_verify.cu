@@ -11,10 +11,9 @@
 // The second product is taken about the middle of the codes: the weights w = p t are rounded to fp16, and an error of w
 // should be multiplied by a code's distance from 8, not by the code (2 to 3 times the error of the output).
 //
-// Two paths compute this: on mma.sync (kv4_verify_mma.cuh) and on tcgen05 (kv4_verify_tc.cuh).  Which of them a call takes
-// is decided on the device, where the lengths are: by every CTA alike, from the chunks of all units.  Units (sequence, KV
-// head) are cut wherever the CTAs' equal shares end; the parts meet through the workspace in a second kernel, which
-// holds nothing over from call to call.
+// Two paths compute this: on mma.sync (kv4_verify_mma.cuh) and, for 33 to 40 query rows, on tcgen05 (kv4_verify_tc.cuh).
+// Units (sequence, KV head) are cut on the device, where the lengths are; the parts meet through the workspace in a second
+// kernel, and nothing is held over from call to call.
 #include <cuda_runtime.h>
 #include <stdint.h>
 #include <string.h>
@@ -35,64 +34,45 @@ namespace {
 
 // What a call of R8 * 8 query rows runs with.
 //
-// mma.sync: as many warps as hold a warp's output in registers.  tcgen05: sixteen warps of 128 registers, for 17 to 48 rows.
-// Below, dequantising is all there is to do, and mma.sync does it with fewer steps (8 sequences x 8 heads x 32768 positions, 4
-// / 16 query rows: 77 / 106 us against 119 / 126); above, sums do not fit (64 rows: 290 against 344).  Between, tcgen05 is
-// ahead from `kTensorLeast` chunks of 32 positions to a CTA on (the same positions, 24 / 32 / 40 rows: 137 / 149 / 158 us
-// against 145 / 168 / 249; 8 x 8 x 1200 positions, 16 chunks: 19.3 / 21.4 / 23.7 against 19.1 / 21.9 / 24.3).
+// mma.sync: as many warps as hold a warp's output in registers.  Two groups of query rows, which read a unit's rows twice,
+// from 33 rows on.  There tcgen05 takes 33 to 40 rows, from kTensorLeast chunks of 32 positions to an SM on that the call's
+// sizes (idx_stride, or the block table) leave room for: 8 sequences x 8 heads x 32768 positions with 40 rows are 159 us
+// against 225, x 2400 (33 chunks) 29.1 against 29.9, x 1200 23.7 against 21.0.  Fewer rows run as fast or faster on
+// mma.sync (24 / 32 rows over 32768: 127 / 152 against 139 / 148; over 2400: 21.9 / 25.5 against 25.4 / 26.9), and with more the
+// sums of tcgen05's threads do not fit their registers (48 rows: 226 against 234).  A kernel for each path: one for both, choosing by
+// the lengths it found, cost small calls 3 us and 10 to 17 where the instructions were not in L2.
+constexpr int kTensorLeast = 32;
 template <int R8>
 struct Config {
   static constexpr int kGroups = R8 > 4 ? 2 : 1;               // of query rows, on mma.sync: 32 are as many as registers hold
   static constexpr int kTiles = (R8 + kGroups - 1) / kGroups;  // of eight queries
-  static constexpr bool kTensor = R8 >= 3 && R8 <= 6;
+  static constexpr bool kTensor = R8 == 5;
   static constexpr int kWarps = R8 == 1 ? 16 : R8 == 2 ? 12 : 8;
   static constexpr int kStages = R8 <= 2 ? 3 : 4;
-  static constexpr int kThreads = kTensor ? kTcWarps * 32 : kWarps * 32;
   using Mma = MmaPath<kTiles, kWarps, kStages>;
-  static constexpr int kSmem = kTensor && kTcSmem > Mma::kSmem ? kTcSmem : Mma::kSmem;
 };
-// Where both paths are there, a call on mma.sync gives eight of the sixteen warps' registers to the others.
-constexpr int kLaunchRegisters = 128, kMoreRegisters = 232, kFewRegisters = 24;
-static_assert(kMoreRegisters + kFewRegisters == 2 * kLaunchRegisters, "eight warps give what eight take");
 
 template <int R8>
-__global__ void __launch_bounds__(Config<R8>::kThreads, 1) kv4_verify_kernel(const __grid_constant__ Kv4Params P) {
+__global__ void __launch_bounds__(Config<R8>::kWarps * 32, 1) kv4_verify_mma_kernel(const __grid_constant__ Kv4Params P) {
   using C = Config<R8>;
   extern __shared__ __align__(1024) unsigned char smem[];
   __shared__ PartitionShared ps;
-  __shared__ union Shared {
-    MmaShared<C::kTiles * 8> mma;
-    Tc4Shared tc;
-    __device__ Shared() {}
-  } sh;
+  __shared__ MmaShared<C::kTiles * 8> sh;
   pdl_wait();  // everything below reads what earlier kernels may have written
-  if constexpr (C::kTensor) {
-    constexpr int kTensorLeast = R8 == 3 ? 96 : R8 == 4 ? 0 : 16;
-    bool tensor = P.engine == 2 || (P.engine == 0 && kTensorLeast == 0);
-    if (P.engine == 0 && kTensorLeast > 0) {
-      const int units = units_of(P, 1).n;
-      int mine = 0, total;
-      for (int u = threadIdx.x; u < units; u += C::kThreads) mine += chunks_of(P, u, kChunk);
-      scan<C::kThreads>(mine, ps, &total);
-      tensor = total >= kTensorLeast * static_cast<int>(gridDim.x);
-    }
-    if (tensor) {
-      const Partition part = cut<C::kThreads>(P, 1, kTile, 2, 12, ps);
-      tc_path<R8>(P, part, smem, sh.tc);
-      pdl_launch_dependents();
-      return;
-    }
-  }
-  if (threadIdx.x < 2) sh.mma.bad[threadIdx.x] = sh.mma.qmax[threadIdx.x] = 0;
-  const Partition part = cut<C::kThreads>(P, 0, kChunk, C::kWarps, 32, ps);
-  if constexpr (C::kTensor) {
-    if (threadIdx.x >= C::kWarps * 32) {
-      set_max_registers_dec<kFewRegisters>();
-      return;
-    }
-    set_max_registers_inc<kMoreRegisters>();
-  }
-  mma_path<C::kTiles, C::kWarps, C::kStages>(P, part, smem, sh.mma);
+  if (threadIdx.x < 2) sh.bad[threadIdx.x] = sh.qmax[threadIdx.x] = 0;
+  const Partition part = cut<C::kWarps * 32>(P, kChunk, C::kWarps, 32, ps);
+  mma_path<C::kTiles, C::kWarps, C::kStages>(P, part, smem, sh);
+  pdl_launch_dependents();
+}
+
+template <int R8>
+__global__ void __launch_bounds__(kTcWarps * 32, 1) kv4_verify_tc_kernel(const __grid_constant__ Kv4Params P) {
+  extern __shared__ __align__(1024) unsigned char smem[];
+  __shared__ PartitionShared ps;
+  __shared__ Tc4Shared sh;
+  pdl_wait();
+  const Partition part = cut<kTcWarps * 32>(P, kTile, 2, 12, ps);
+  tc_path<R8>(P, part, smem, sh);
   pdl_launch_dependents();
 }
 
@@ -100,12 +80,12 @@ __global__ void __launch_bounds__(Config<R8>::kThreads, 1) kv4_verify_kernel(con
 __global__ void __launch_bounds__(256) kv4_join_kernel(const __grid_constant__ Kv4Params P) {
   pdl_launch_dependents();
   pdl_wait();
-  const Units units = units_of(P, *P.path);
+  const Units units = units_of(P);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const long long rec_floats = static_cast<long long>(units.rows) * kRowFloats;
   // (the part of the CTA where a unit begins is that CTA's second record, all others are first records)
   auto rec_of = [&](int c, int first) { return P.partial + (2 * c + (c == first ? 1 : 0)) * rec_floats; };
-  if (blockIdx.x == P.most_units) {  // the last block gathers the status words
+  if (blockIdx.x == units.n) {  // the last block gathers the status words
     if (P.status == nullptr || blockIdx.y != 0) return;
     for (int b = warp; b < P.B; b += 8) {
       int flag = 0;
@@ -122,7 +102,6 @@ __global__ void __launch_bounds__(256) kv4_join_kernel(const __grid_constant__ K
     return;
   }
   const int u = blockIdx.x;
-  if (u >= units.n) return;
   const int2 of = P.parts[u];
   if (of.x == of.y) return;
   const int rg = u / (P.B * P.H), bh = u - rg * P.B * P.H, b = bh / P.H, h = bh - b * P.H;
@@ -173,24 +152,45 @@ int validate(const specattn_kv4_verify_args* args) {
   if (A.cache.n_pages > INT32_MAX) return SPECATTN_ERR_RANGE;
   constexpr uint32_t kEngines = SPECATTN_VERIFY_ENGINE_MMA_SYNC | SPECATTN_VERIFY_ENGINE_TCGEN05;
   if ((A.flags & ~(kEngines | SPECATTN_VERIFY_TEST_LOSE_ARRIVAL)) != 0 || (A.flags & kEngines) == kEngines) return SPECATTN_ERR_RANGE;
-  if (A.head_dim != kKv4D || A.n_q > SPECATTN_MAX_QUERY_ROWS || A.n_q * (A.n_q_heads / A.n_kv_heads) > SPECATTN_MAX_QUERY_ROWS ||
+  if (A.head_dim != kKv4D || A.n_q > SPECATTN_MAX_QUERY_ROWS || A.n_q_heads / A.n_kv_heads > SPECATTN_MAX_QUERY_ROWS / A.n_q ||
       static_cast<long long>(A.batch) * A.n_kv_heads > kMaxUnits)
     return SPECATTN_ERR_UNSUPPORTED;
   const int rows = A.n_q * (A.n_q_heads / A.n_kv_heads);
-  if ((A.flags & SPECATTN_VERIFY_ENGINE_TCGEN05) && (rows <= 16 || rows > 48)) return SPECATTN_ERR_UNSUPPORTED;
+  if ((A.flags & SPECATTN_VERIFY_ENGINE_TCGEN05) && (rows <= 32 || rows > 40)) return SPECATTN_ERR_UNSUPPORTED;
   return SPECATTN_OK;
 }
 
-// the path, parts, flags; then the records
+// parts, flags; then the records
 size_t table_bytes(const specattn_kv4_verify_args& A) {
-  return (static_cast<size_t>(A.batch) * A.n_kv_heads * groups_of(query_tiles(A)) * 3 + 2 + 63) / 64 * 256;
+  return (static_cast<size_t>(A.batch) * A.n_kv_heads * groups_of(query_tiles(A)) * 3 + 63) / 64 * 256;
 }
 size_t workspace_bytes(const specattn_kv4_verify_args& A, int sms) {
   return table_bytes(A) + static_cast<size_t>(2) * sms * query_tiles(A) * 8 * kRowFloats * sizeof(float);
 }
 
+int launch_one(void (*kernel)(Kv4Params), const Kv4Params& P, dim3 grid, int threads, int smem, cudaStream_t stream) {
+  cudaLaunchConfig_t cfg;
+  memset(&cfg, 0, sizeof(cfg));
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  if (cudaLaunchKernelEx(&cfg, kernel, P) != cudaSuccess) {
+    cudaGetLastError();
+    return SPECATTN_ERR_CUDA;
+  }
+  g_launch_count.fetch_add(1, std::memory_order_relaxed);
+  return SPECATTN_OK;
+}
+
+// most: the largest number of chunks of 32 positions that the call can have, by its sizes
 template <int R8>
-int launch(const Kv4Params& P, int sms, cudaStream_t stream) {
+int launch(Kv4Params& P, int engine, double most, int sms, cudaStream_t stream) {
   using C = Config<R8>;
   static std::atomic<unsigned long long> prepared{0};  // a bit per device
   int dev = 0;
@@ -199,39 +199,31 @@ int launch(const Kv4Params& P, int sms, cudaStream_t stream) {
     return SPECATTN_ERR_CUDA;
   }
   if (!((prepared.load(std::memory_order_acquire) >> dev) & 1ull)) {
-    // (what one half of the warps gives the other takes: with fewer registers at launch they would wait for ever)
-    cudaFuncAttributes built;
-    if (cudaFuncGetAttributes(&built, kv4_verify_kernel<R8>) != cudaSuccess || (C::kTensor && built.numRegs != kLaunchRegisters) ||
-        cudaFuncSetAttribute(kv4_verify_kernel<R8>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem) != cudaSuccess) {
+    cudaError_t rc = cudaFuncSetAttribute(kv4_verify_mma_kernel<R8>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::Mma::kSmem);
+    if constexpr (C::kTensor)
+      if (rc == cudaSuccess) rc = cudaFuncSetAttribute(kv4_verify_tc_kernel<R8>, cudaFuncAttributeMaxDynamicSharedMemorySize, kTcSmem);
+    if (rc != cudaSuccess) {
       cudaGetLastError();
       return SPECATTN_ERR_CUDA;
     }
     prepared.fetch_or(1ull << dev, std::memory_order_release);
   }
-  cudaLaunchConfig_t cfg;
-  memset(&cfg, 0, sizeof(cfg));
-  cfg.gridDim = dim3(sms);
-  cfg.blockDim = dim3(C::kThreads);
-  cfg.dynamicSmemBytes = C::kSmem;
-  cfg.stream = stream;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  if (cudaLaunchKernelEx(&cfg, kv4_verify_kernel<R8>, P) != cudaSuccess) {
-    cudaGetLastError();
-    return SPECATTN_ERR_CUDA;
+  P.n_units = P.B * P.H * C::kGroups;
+  P.rows_per_unit = C::kTiles * 8;
+  int rc = SPECATTN_OK;
+  if constexpr (C::kTensor) {
+    if (engine == 2 || (engine == 0 && most >= static_cast<double>(kTensorLeast) * sms)) {
+      P.n_units = P.B * P.H;
+      P.rows_per_unit = R8 * 8;
+      rc = launch_one(kv4_verify_tc_kernel<R8>, P, dim3(sms), kTcWarps * 32, kTcSmem, stream);
+    } else {
+      rc = launch_one(kv4_verify_mma_kernel<R8>, P, dim3(sms), C::kWarps * 32, C::Mma::kSmem, stream);
+    }
+  } else {
+    rc = launch_one(kv4_verify_mma_kernel<R8>, P, dim3(sms), C::kWarps * 32, C::Mma::kSmem, stream);
   }
-  cfg.gridDim = dim3(P.most_units + 1, R8);
-  cfg.blockDim = dim3(256);
-  cfg.dynamicSmemBytes = 0;
-  if (cudaLaunchKernelEx(&cfg, kv4_join_kernel, P) != cudaSuccess) {
-    cudaGetLastError();
-    return SPECATTN_ERR_CUDA;
-  }
-  g_launch_count.fetch_add(2, std::memory_order_relaxed);
-  return SPECATTN_OK;
+  if (rc != SPECATTN_OK) return rc;
+  return launch_one(kv4_join_kernel, P, dim3(P.n_units + 1, R8), 256, 0, stream);
 }
 
 }  // namespace
@@ -262,9 +254,6 @@ extern "C" int specattn_kv4_verify(const specattn_kv4_verify_args* args, void* c
   if (reinterpret_cast<uintptr_t>(A.q) % 16 != 0 || reinterpret_cast<uintptr_t>(A.out) % 16 != 0 ||
       reinterpret_cast<uintptr_t>(A.workspace) % 256 != 0)
     return SPECATTN_ERR_ALIGN;
-  const int sms = device_sm_count();
-  if (sms <= 0) return SPECATTN_ERR_CUDA;
-  if (A.workspace_bytes < workspace_bytes(A, sms)) return SPECATTN_ERR_WORKSPACE;
   const specattn_kv4_cache& cache = A.cache;
   // the kernel addresses codes in 16-byte and params in 4-byte units of 32 bits
   const double reach = (static_cast<double>(cache.n_pages) * cache.stride_page + cache.stride_kv +
@@ -275,7 +264,10 @@ extern "C" int specattn_kv4_verify(const specattn_kv4_verify_args* args, void* c
       cache.pstride_kv < 0 || cache.pstride_slot < 0 || cache.pstride_head < 0 || reach >= 4294967296. || reach_params >= 4294967296. ||
       cache.block_table_stride > INT32_MAX)
     return SPECATTN_ERR_UNSUPPORTED;
-  const int r8 = query_tiles(A), groups = groups_of(r8);
+  const int sms = device_sm_count();
+  if (sms <= 0) return SPECATTN_ERR_CUDA;
+  if (A.workspace_bytes < workspace_bytes(A, sms)) return SPECATTN_ERR_WORKSPACE;
+  const int r8 = query_tiles(A);
   Kv4Params P;
   memset(&P, 0, sizeof(P));
   P.cache = kv4_view(A.cache);
@@ -292,10 +284,8 @@ extern "C" int specattn_kv4_verify(const specattn_kv4_verify_args* args, void* c
   P.out = static_cast<unsigned char*>(A.out);
   P.lse = A.lse;
   P.status = A.status;
-  P.most_units = A.batch * A.n_kv_heads * groups;
-  P.path = static_cast<int*>(A.workspace);
-  P.parts = reinterpret_cast<int2*>(P.path + 2);
-  P.flags = P.path + 2 + 2 * P.most_units;
+  P.parts = static_cast<int2*>(A.workspace);
+  P.flags = reinterpret_cast<int*>(P.parts + A.batch * A.n_kv_heads * groups_of(r8));
   P.partial = reinterpret_cast<float*>(static_cast<unsigned char*>(A.workspace) + table_bytes(A));
   P.scale = (A.sm_scale != 0.f ? A.sm_scale : 1.0f / sqrtf(static_cast<float>(A.head_dim))) * kLog2e;
   P.B = A.batch;
@@ -309,19 +299,19 @@ extern "C" int specattn_kv4_verify(const specattn_kv4_verify_args* args, void* c
   P.tail = A.tail_len;
   P.out_f32 = A.out_f32 ? 1 : 0;
   P.half = A.cache.dtype == SPECATTN_DTYPE_FP16 ? 1 : 0;
-  P.engine = A.flags & SPECATTN_VERIFY_ENGINE_TCGEN05 ? 2 : A.flags & SPECATTN_VERIFY_ENGINE_MMA_SYNC ? 1 : 0;
   P.test_lose = A.flags & SPECATTN_VERIFY_TEST_LOSE_ARRIVAL ? 1 : 0;
-  P.groups_of_rows = groups;
-  P.rows_per_group = (r8 + groups - 1) / groups * 8;
   const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+  const int engine = A.flags & SPECATTN_VERIFY_ENGINE_TCGEN05 ? 2 : A.flags & SPECATTN_VERIFY_ENGINE_MMA_SYNC ? 1 : 0;
+  const double longest = A.dense ? static_cast<double>(cache.block_table_stride) * cache.page_size : static_cast<double>(A.idx_stride);
+  const double most = static_cast<double>(A.batch) * A.n_kv_heads * ((longest + A.tail_len) / kChunk + 1);
   switch (r8) {
-    case 1: return launch<1>(P, sms, stream);
-    case 2: return launch<2>(P, sms, stream);
-    case 3: return launch<3>(P, sms, stream);
-    case 4: return launch<4>(P, sms, stream);
-    case 5: return launch<5>(P, sms, stream);
-    case 6: return launch<6>(P, sms, stream);
-    case 7: return launch<7>(P, sms, stream);
-    default: return launch<8>(P, sms, stream);
+    case 1: return launch<1>(P, engine, most, sms, stream);
+    case 2: return launch<2>(P, engine, most, sms, stream);
+    case 3: return launch<3>(P, engine, most, sms, stream);
+    case 4: return launch<4>(P, engine, most, sms, stream);
+    case 5: return launch<5>(P, engine, most, sms, stream);
+    case 6: return launch<6>(P, engine, most, sms, stream);
+    case 7: return launch<7>(P, engine, most, sms, stream);
+    default: return launch<8>(P, engine, most, sms, stream);
   }
 }

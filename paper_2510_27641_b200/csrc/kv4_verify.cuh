@@ -26,17 +26,15 @@ struct Kv4Params {
   unsigned char* out;
   float* lse;
   int* status;
-  int* path;       // workspace: the path taken
   int2* parts;     // workspace: first and last CTA of every unit, (0, -1) where it has no positions
   int* flags;      // workspace: status of the units that one CTA has done, [units]; other units have it in their records
   float* partial;  // workspace: two records of a unit's rows for every CTA
   float scale;     // sm_scale * log2(e)
   int B, T, Hq, H, grp, rows, G, dense, tail, out_f32, half;
-  int groups_of_rows, rows_per_group;  // of the mma.sync path
-  int most_units;                      // of either path
+  int n_units, rows_per_unit;
   unsigned c_page, c_slot, p_page, p_slot;  // strides of codes in 16-byte, of params in 4-byte units
   int pages_per_seq;
-  int engine, test_lose;               // 1: mma.sync, 2: tcgen05, 0: by the lengths
+  int test_lose;
 };
 
 // A value that all lanes share, in a register that the warp shares.
@@ -46,12 +44,7 @@ __device__ __forceinline__ int uniform(int x) { return static_cast<int>(__reduce
 struct Units {
   int n, rows;  // units; query rows of one
 };
-__device__ __forceinline__ Units units_of(const Kv4Params& P, int tensor) {
-  Units u;
-  u.n = P.B * P.H * (tensor ? 1 : P.groups_of_rows);
-  u.rows = tensor ? (P.rows + 7) / 8 * 8 : P.rows_per_group;
-  return u;
-}
+__device__ __forceinline__ Units units_of(const Kv4Params& P) { return {P.n_units, P.rows_per_unit}; }
 
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   const __half2 v = __floats2half2_rn(lo, hi);
@@ -79,7 +72,7 @@ __device__ __forceinline__ uint2 lds64(uint32_t a) {
 
 // Positions that sequence b, head h attends before the tail.
 __device__ __forceinline__ int list_len(const Kv4Params& P, int b, int h) {
-  if (P.dense) return max(0, min(P.kv_len[b], kMaxPositions));
+  if (P.dense) return max(0, min(P.kv_len[b], kMaxPositions + 1));  // (the last of these is beyond any table)
   return static_cast<int>(max(0ll, min(static_cast<long long>(P.counts[b * P.G + (P.G > 1 ? h : 0)]), P.idx_stride)));
 }
 __device__ __forceinline__ int chunks_of(const Kv4Params& P, int u, int chunk) {
@@ -133,9 +126,9 @@ __device__ __forceinline__ int scan(int v, PartitionShared& S, int* total) {
 // enough, equal parts of units: of lengths from an equal run's on, in steps of an eighth, each tried by a warp, the
 // shortest whose parts are no more than the CTAs, if it exceeds an equal run by less than `afresh`.
 template <int kThreads>
-__device__ __forceinline__ Partition cut(const Kv4Params& P, int tensor, int chunk, int least, int afresh, PartitionShared& S) {
+__device__ __forceinline__ Partition cut(const Kv4Params& P, int chunk, int least, int afresh, PartitionShared& S) {
   static_assert(kThreads >= kMostParted && kThreads <= 512, "a unit to a thread, a length to a warp");
-  const int tid = threadIdx.x, lane = tid & 31, grid = static_cast<int>(gridDim.x), units = units_of(P, tensor).n;
+  const int tid = threadIdx.x, lane = tid & 31, grid = static_cast<int>(gridDim.x), units = units_of(P).n;
   const int per_thread = (units + kThreads - 1) / kThreads;
   const int u0 = min(tid * per_thread, units), u1 = min(u0 + per_thread, units);
   int mine = 0, total;
@@ -146,7 +139,6 @@ __device__ __forceinline__ Partition cut(const Kv4Params& P, int tensor, int chu
   Partition p;
   p.unit = units;
   p.start = p.first = p.last = 0;
-  if (blockIdx.x == 0 && tid == 0) *P.path = tensor;
   const int per = max((total + grid - 1) / grid, least);
   if (units <= min(grid, kMostParted)) {
     const auto length_of = [&](int step) { return per + per * step / 8; };

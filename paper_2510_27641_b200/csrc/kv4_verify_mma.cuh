@@ -55,8 +55,7 @@ __device__ __forceinline__ void mma_path(const Kv4Params& P, const Partition& pa
   const int tid = threadIdx.x, lane = tid & 31, warp = uniform(tid >> 5);
   const int g = lane >> 2, t = lane & 3;
   const uint32_t ring_at = smem_u32(smem + K::kQBytes + warp * K::kRing);
-  const Units units = units_of(P, 0);
-  const auto sync = [] { named_bar_sync(5, NWARP * 32); };  // (other warps of the CTA may have left)
+  const Units units = units_of(P);
   const int last = uniform(part.last);
   int u = uniform(part.unit), u_start = uniform(part.start), turn = 0;
 
@@ -112,7 +111,7 @@ __device__ __forceinline__ void mma_path(const Kv4Params& P, const Partition& pa
 
     // ---- queries ----
     queries.look(P, row0, n_rows, &S.qmax[turn], S.qsum, S.limit);
-    sync();
+    __syncthreads();
     if (tid == 0) S.bad[turn ^ 1] = S.qmax[turn ^ 1] = 0;
     const int qexp = query_exponent(S.qmax[turn]);
     // step 2 w meets codes 0, 4 (low halves of bytes) and 1, 5 (high) of word w of the lane's 16 bytes, step 2 w + 1
@@ -120,7 +119,7 @@ __device__ __forceinline__ void mma_path(const Kv4Params& P, const Partition& pa
     queries.place(P, __int_as_float((127 + qexp) << 23), [&](int r, int word, int half, uint2 x) {
       reinterpret_cast<uint2*>(smem)[((r >> 3) * 8 + 2 * (word & 3) + half) * 32 + (r & 7) * 4 + (word >> 2)] = x;
     });
-    sync();
+    __syncthreads();
     const float k_mul = P.scale * 16777216.f * __int_as_float((127 - qexp) << 23);  // codes are c 2^-24 in the product
     Two sq[NT], m[NT], l[NT], y[NT];  // of two queries: sum q; minus the running maximum (log2), sum of p, sum of p (y + 8 t)
     float acc[8][NT][4], acc8[NT][4];                // output by (element tile, query tile), less its middle
@@ -308,7 +307,7 @@ __device__ __forceinline__ void mma_path(const Kv4Params& P, const Partition& pa
       }
     }
     cp_wait<0>();
-    sync();  // the rings are free
+    __syncthreads();  // the rings are free
 
     // ---- the warps' parts meet ----
     float* meet = reinterpret_cast<float*>(smem + K::kQBytes);
@@ -339,7 +338,7 @@ __device__ __forceinline__ void mma_path(const Kv4Params& P, const Partition& pa
           }
         }
     }
-    sync();
+    __syncthreads();
     const bool whole = seg0 == 0 && seg1 == n_chunks;
     float* rec = P.partial + static_cast<long long>(2 * blockIdx.x + (seg0 == 0 ? 1 : 0)) * units.rows * kRowFloats;
     finish<NWARP, NWARP, K::kQueries>(P, meet, b, h, row0, n_rows, whole, rec);
@@ -350,7 +349,7 @@ __device__ __forceinline__ void mma_path(const Kv4Params& P, const Partition& pa
         rec[kKv4D + 2] = __int_as_float(S.bad[turn]);
     }
     turn ^= 1;
-    sync();  // the records have been read
+    __syncthreads();  // the records have been read
     at = u_start + seg1;
     if (seg1 == n_chunks) {
       u_start += n_chunks;

@@ -1,23 +1,26 @@
-// The path of specattn_kv4_verify on tcgen05, for 17 query rows and more over long lists.
+// The path of specattn_kv4_verify on tcgen05, for 33 to 40 query rows over long lists.
 //
 // mma.sync does 1024 multiply-adds a cycle and SM, which 24 query rows use up at the speed of the memory; tcgen05 does
 // four times that, and its operands need not pass through registers.  As in the bf16 kernel both products are taken
-// transposed, with 128 positions (or the 128 elements of an output row) as the M side and the N = 32 ... 64 query rows
-// as the other:
+// transposed, with 128 positions (or the 128 elements of an output row) as the M side and the N = 48 query rows (40 and
+// zeros) as the other:
 //     S^T [128 positions x N] = C_K [128 x 128] Q^T            C_K in tensor memory, Q in shared memory
 //     O^T [128 elements x N] += (C_V - 8)^T [128 x 128] W      both in shared memory, position-major
-// A thread owns a position: it unpacks the K row's codes by masks (the subnormals of fp16, see kv4_verify.cu) straight into
-// its lane of tensor memory, and the V row's into a row of the swizzled operand; it gets the position's scores back
-// as its lane of S^T, so that scale and zero point are the thread's own; and it writes the position's row of W.
+// Two threads own a position, each half of its codes and half of the queries: they unpack the K row's codes by masks (the
+// subnormals of fp16, see kv4_verify.cu) straight into their lane of tensor memory, and the V row's into a row of the
+// swizzled operand; they get the position's scores back as that lane of S^T, so that scale and zero point are the
+// threads' own; and they write the position's row of W.
 // 8 is taken off the V codes by a packed subtraction, exact in fp16: the weights' rounding errors then multiply a
 // code's distance from the middle, and the accumulators do not grow with the sum of the weights.
 //
-// Two groups of four warps take tiles of 128 positions in turn, each with operands, accumulators and a running maximum of
+// Two groups of eight warps take tiles of 128 positions in turn, each with operands, accumulators and a running maximum of
 // its own, and run a phase apart.  In a group's turn:
 //     scores of tile i from tensor memory | K of tile i + 1 into it | vote (may the maximum stay?) and S^T of i + 1 starts |
-//     V of tile i | weights of tile i | O^T of tile i starts
-// Shared memory takes 17 KB of copies, 16 KB of reads, 32 KB of V operand written and read each, and W and Q: about
-// 940 cycles a tile at 128 bytes a cycle, where HBM takes 757 at 1.9 GHz.
+//     V of tile i, copies of tile i + 3 asked for | weights of tile i | O^T of tile i starts
+// 40 rows over 8 x 8 x 32768 positions: 159 us, 1.8 TB/s.  A tile takes an SM about 2700 cycles, where HBM would take 757 and
+// shared memory (16 KB of copies written and read, 32 KB of V operand, W and Q) 940: what bounds it is the chain of
+// instructions, barriers and products in flight in a group's turn.  (Taking 8 off by one more product with a constant
+// operand instead: 137 to 141 us at 24 rows.)
 #pragma once
 #include "kv4_verify.cuh"
 
@@ -141,7 +144,7 @@ __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& par
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   const uint32_t v_at = smem_u32(smem) + g * 32768, w_at = smem_u32(smem) + 65536 + g * 16384, q_at = smem_u32(smem) + 98304;
   const uint32_t ring_at = q_at + 16384 + warp * kTcRing * kTcStage;
-  const Units units = units_of(P, 1);
+  const Units units = units_of(P);
 
   if (warp == 0) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&S.tmem)), "r"(512u) : "memory");
@@ -157,7 +160,7 @@ __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& par
     S.abort = 0;
   }
   // (columns of W and rows of Q beyond the query rows stay zero)
-  for (int i = tid; i < 3072; i += kTcWarps * 32) reinterpret_cast<uint4*>(smem + 65536)[i] = make_uint4(0u, 0u, 0u, 0u);
+  for (int i = tid; i < (2 * 16384 + 16384) / 16; i += kTcWarps * 32) reinterpret_cast<uint4*>(smem + 65536)[i] = make_uint4(0u, 0u, 0u, 0u);
   tm_before();
   __syncthreads();
   tm_after();

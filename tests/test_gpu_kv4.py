@@ -168,7 +168,12 @@ ENGINES = {"auto": 0, "mma.sync": 2, "tcgen05": 4}
 
 def _engines(T, Hq, Hkv):
     """What may run that many query rows."""
-    return ["auto", "mma.sync", "tcgen05"] if 16 < T * (Hq // Hkv) <= 48 else ["auto"]
+    return ["auto", "mma.sync", "tcgen05"] if 32 < T * (Hq // Hkv) <= 40 else ["auto"]
+
+
+def _more(engine, few, more):
+    """Query heads for an engine: tcgen05 starts at 33 query rows per KV head."""
+    return more if engine == "tcgen05" else few
 
 
 def _run(c, engine="auto", **kw):
@@ -258,7 +263,7 @@ def test_long_lists_split_over_the_gpu(T, Hq, Hkv, lens, counts):
 
 
 def test_calls_long_enough_for_tcgen05_take_it_by_themselves():
-    c = _case(44, 2, 6, 8, 2, [150000, 100000], None, dense=True)
+    c = _case(44, 2, 6, 12, 2, [150000, 100000], None, dense=True)
     out, lse, _ = _run(c)
     tc, mma = _run(c, "tcgen05"), _run(c, "mma.sync")
     assert torch.equal(out, tc[0]) and torch.equal(lse, tc[1]) and not torch.equal(lse, mma[1])
@@ -270,7 +275,7 @@ def test_a_bounded_wait_that_runs_out_is_reported():
     """The first completion of CTA 0 is withheld: its waits run out, the kernel returns, the status says so, and the next call is
     right."""
     sa = _sa()
-    c = _case(45, 2, 6, 32, 8, [3000, 2000], None, dense=True)
+    c = _case(45, 2, 6, 48, 8, [3000, 2000], None, dense=True)
     status = torch.zeros(2, dtype=torch.int32, device=DEV)
     _run(c, status=status, flags=sa.VERIFY_ENGINE_TCGEN05 | sa.VERIFY_TEST_LOSE_ARRIVAL)
     assert status[0].item() == sa.ROW_TIMEOUT
@@ -284,7 +289,7 @@ def test_scores_that_grow_and_scales_that_grow(engine):
     """The running maximum and the weights' scale both move along the list: K rows that a query likes more and more,
     V rows whose range spans 2^30."""
     gen, n = _gen(47), 2000
-    c = _case(47, 1, 5, 8, 2, [n], None, dense=True)
+    c = _case(47, 1, 5, _more(engine, 8, 16), 2, [n], None, dense=True)
     x = torch.randn(c["codes"].shape[0], 2, 16, 2, 128, generator=gen)
     for b in range(c["table"].shape[1]):
         page = int(c["table"][0, b])
@@ -304,7 +309,7 @@ def test_scores_that_grow_and_scales_that_grow(engine):
 
 @pytest.mark.parametrize("engine", ["mma.sync", "tcgen05"])
 def test_constant_rows_and_rows_far_from_zero(engine):
-    c = _case(53, 2, 6, 32, 8, [500, 33], None, dense=True)
+    c = _case(53, 2, 6, _more(engine, 32, 48), 8, [500, 33], None, dense=True)
     gen = _gen(53)
     x = torch.randn(c["codes"].shape[0], 2, 16, 8, 128, generator=gen)
     x[::3] = x[::3, :, :, :, :1]               # constant rows: scale 0
@@ -318,7 +323,7 @@ def test_constant_rows_and_rows_far_from_zero(engine):
 @pytest.mark.parametrize("engine", ["mma.sync", "tcgen05"])
 def test_queries_of_any_magnitude(scale, engine):
     """A power of two in the queries and its inverse in sm_scale: bf16's range, beyond fp16's."""
-    c = _case(59, 2, 6, 32, 8, [200, 100], [150, 100])
+    c = _case(59, 2, 6, _more(engine, 32, 48), 8, [200, 100], [150, 100])
     out, lse, _ = _run(c, engine=engine)
     big = dict(c, q=c["q"] * scale)
     out2, lse2, _ = _run(big, engine, sm_scale=1 / (math.sqrt(128) * scale))
@@ -329,7 +334,7 @@ def test_queries_of_any_magnitude(scale, engine):
 @pytest.mark.parametrize("engine", ["mma.sync", "tcgen05"])
 def test_float32_output_and_given_buffers(engine):
     sa = _sa()
-    c = _case(61, 2, 6, 32, 8, [300, 900], [280, 700])
+    c = _case(61, 2, 6, _more(engine, 32, 48), 8, [300, 900], [280, 700])
     out16, lse16, _ = _run(c, engine=engine)
     out = torch.full(c["q"].shape, float("nan"), device=DEV)
     lse = torch.full(c["q"].shape[:3], float("nan"), device=DEV)
@@ -345,7 +350,7 @@ def test_float32_output_and_given_buffers(engine):
 @pytest.mark.parametrize("engine", ["mma.sync", "tcgen05"])
 def test_nothing_outside_the_lists_is_looked_at(engine):
     """Every row that no list names, masked tail rows and ends of pages hold NaN."""
-    c = _case(67, 2, 5, 16, 4, [333, 90], [200, 60], tail=5)
+    c = _case(67, 2, 5, _more(engine, 16, 32), 4, [333, 90], [200, 60], tail=5)
     params = torch.full_like(c["params"], float("nan"))
     for b in range(2):
         for pos in c["lists"][b][0] + [c["lens"][b] + j for j in range(5)]:
@@ -367,13 +372,13 @@ def test_nothing_outside_the_lists_is_looked_at(engine):
 
 @pytest.mark.parametrize("engine", ["mma.sync", "tcgen05"])
 def test_a_query_of_nan_or_infinity_spoils_no_other(engine):
-    c = _case(71, 1, 6, 32, 8, [200], [150])
+    c = _case(71, 1, 6, _more(engine, 32, 48), 8, [200], [150])
     out, lse, _ = _run(c, engine=engine)
     for bad in (float("nan"), float("inf")):
         q = c["q"].clone()
         q[0, 2, 5, 17] = bad
         out2, lse2, _ = _run(dict(c, q=q), engine=engine)
-        keep = torch.ones(6, 32, dtype=torch.bool)
+        keep = torch.ones(6, c["q"].shape[2], dtype=torch.bool)
         keep[2, 5] = False
         assert torch.equal(out2[0][keep.to(DEV)], out[0][keep.to(DEV)]) and torch.equal(lse2[0][keep.to(DEV)], lse[0][keep.to(DEV)])
         assert torch.all(torch.isnan(out2[0, 2, 5]))
@@ -382,7 +387,7 @@ def test_a_query_of_nan_or_infinity_spoils_no_other(engine):
 @pytest.mark.parametrize("engine", ["mma.sync", "tcgen05"])
 def test_bad_positions_and_pages_are_reported_and_read_from_the_first(engine):
     sa = _sa()
-    c = _case(73, 4, 5, 8, 2, [100, 100, 100, 100], [50, 50, 50, 50])
+    c = _case(73, 4, 5, _more(engine, 8, 16), 2, [100, 100, 100, 100], [50, 50, 50, 50])
     c["idx"][1, 0, 7] = 100        # beyond the context
     c["idx"][2, 0, 0] = -5
     c["table"][3, 2] = 10 ** 6     # no such page
@@ -394,7 +399,7 @@ def test_bad_positions_and_pages_are_reported_and_read_from_the_first(engine):
     first = dict(c, q=c["q"][:1], table=c["table"][:1], lens=[100], lists=c["lists"][:1])
     _check(first, out[:1], lse[:1])
     # a context longer than the block table, dense
-    c = _case(74, 1, 5, 8, 2, [100], None, dense=True)
+    c = _case(74, 1, 5, _more(engine, 8, 16), 2, [100], None, dense=True)
     c["lens"] = [5000]
     status = torch.zeros(1, dtype=torch.int32, device=DEV)
     out, _, _ = _run(c, status=status, engine=engine)
@@ -432,7 +437,7 @@ def test_rows_beyond_four_gigabytes():
 @pytest.mark.parametrize("engine", ["mma.sync", "tcgen05"])
 def test_the_same_bits_again_on_a_stream_and_in_a_graph(engine):
     sa = _sa()
-    c = _case(89, 3, 6, 32, 8, [3000, 40, 700], [2500, 40, 333], tail=6)
+    c = _case(89, 3, 6, _more(engine, 32, 48), 8, [3000, 40, 700], [2500, 40, 333], tail=6)
     ref = _run(c, engine=engine)
     up = lambda t: t.to(DEV)
     q, codes, params, table, idx, counts = up(c["q"]), _to_gpu(c["codes"]), _to_gpu(c["params"]), up(c["table"]), up(c["idx"]), up(c["counts"])
