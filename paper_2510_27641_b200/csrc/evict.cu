@@ -655,15 +655,21 @@ extern "C" int specattn_evict(const specattn_evict_args* args, void* cuda_stream
   P.n_recent = A.n_recent;
   P.B = A.batch;
   P.G = A.n_groups;
-  // a CTA to 8192 slots, up to eight; no more than the slots need while there are lists enough for all SMs
+  const int sms = device_sm_count();
+  if (sms <= 0) return SPECATTN_ERR_CUDA;
+  // CTAs to a list: enough for 16384 slots or fewer to each (40 lists of 32768, one or two CTAs to an SM are 26 to 29 us; 300
+  // of 20000 whole 95, halved 74); more while every one has an SM to itself and 1024 slots (8 lists of 32768 with 2 / 4 / 8:
+  // 27.6 / 18.8 / 14.8 us, one of 4096 with 1 / 2 / 4 / 8: 12.6 / 11.1 / 10.3 / 10.6)
   int ctas = 1;
-  while (ctas < kEvMaxCluster && ctas * 8192 < A.L && (lists * ctas < 296 || ctas * kEvMaxSlice < A.L)) ctas *= 2;
+  const auto slots = [&] { return (A.L + ctas - 1) / ctas; };
+  while (ctas < kEvMaxCluster && (slots() > 16384 || (lists * ctas * 2 <= sms && slots() >= 2048))) ctas *= 2;
   P.slice = static_cast<int>(((A.L + ctas - 1) / ctas + 3) / 4 * 4);
   P.wide = A.L % 4 == 0 && ((reinterpret_cast<uintptr_t>(A.scores) | reinterpret_cast<uintptr_t>(A.positions) |
                              reinterpret_cast<uintptr_t>(A.scores_out) | reinterpret_cast<uintptr_t>(A.positions_out)) % 16 == 0);
   const size_t smem = static_cast<size_t>(P.slice) * sizeof(uint32_t);
-  // 1024 threads where a CTA has an SM to itself: 8 lists of 32768 18 against 20 us; of 512 two fit, and 256 CTAs run at once
-  const bool many = lists * ctas > device_sm_count();
+  // 1024 threads for many slots on an SM of their own (74 lists of 32768 by halves 26.6 against 29.1 us); of 512 two CTAs fit, and
+  // fewer slots do not fill more (8 lists of 32768 by eighths 14.8 against 15.3, 224 of 2667 15.7 against 23.9)
+  const bool many = slots() < 8192 || lists * ctas > sms;
   const auto kernel = many ? evict_kernel<512> : evict_kernel<1024>;
   static std::atomic<unsigned long long> prepared[2];  // a bit per device
   int dev = 0;
