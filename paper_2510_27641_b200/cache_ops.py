@@ -49,6 +49,21 @@ def _strides(t: torch.Tensor, first: int, last: int):
     return [s if n > 1 else 0 for s, n in zip(t.stride()[first:last], t.shape[first:last])]
 
 
+def _behind(stream, made, device):
+    """What was allocated on the current stream is used on the caller's: whoever had the memory before is done by then, and
+    nobody gets it earlier than that stream is done."""
+    if stream is not None and made:
+        stream.wait_stream(torch.cuda.current_stream(device))
+        for t in made:
+            t.record_stream(stream)
+
+
+def _apart(*tensors):
+    """Tensors that a call writes: no two elements in one place."""
+    for t in tensors:
+        assert t.numel() == 0 or all(s > 0 for s, n in zip(t.stride(), t.shape) if n > 1), "a tensor that is written may not be expanded"
+
+
 def _ints(t: torch.Tensor | None, n: int, what: str):
     """A vector of n 32-bit integers (or None), by address."""
     if t is None:
@@ -97,7 +112,7 @@ def _pages_per_seq(table, pages_per_seq, batch) -> int:
 
 def _rows(name, k, v, codes, params, start, n, block_table, pages_per_seq, status, stream):
     index = _device(k, v, codes, params, start, n, block_table, status)
-    key = (k.shape, k.stride(), k.dtype, v.shape, v.stride(), v.dtype) + _cache_key(codes, params, block_table, pages_per_seq)
+    key = (name, k.shape, k.stride(), k.dtype, v.shape, v.stride(), v.dtype) + _cache_key(codes, params, block_table, pages_per_seq)
 
     def make():
         b, t, h, d = k.shape
@@ -107,6 +122,7 @@ def _rows(name, k, v, codes, params, start, n, block_table, pages_per_seq, statu
         a.batch, a.n_tokens, a.n_kv_heads, a.head_dim = b, t, h, d
         _fill_cache(a.cache, codes, params, block_table, pages_per_seq, b)
         assert k.dtype is params.dtype and v.dtype is params.dtype, "k, v: of the type of params"
+        _apart(*((codes, params) if name.endswith("append") else (k, v)))
         a.k_stride_batch, a.k_stride_token, a.k_stride_head = _strides(k, 0, 3)
         a.v_stride_batch, a.v_stride_token, a.v_stride_head = _strides(v, 0, 3)
         return a, a.cache, C.byref(a), b
@@ -139,10 +155,7 @@ def kv4_read(codes: torch.Tensor, params: torch.Tensor, start: torch.Tensor, *, 
     if k is None or v is None:
         shape = (start.shape[0], int(n_tokens), codes.shape[3], 128) if k is None and v is None else (v if k is None else k).shape
         made = [torch.zeros(shape, dtype=params.dtype, device=params.device) for x in (k, v) if x is None]
-        if stream is not None:   # filled on the current stream, written on the caller's
-            stream.wait_stream(torch.cuda.current_stream(params.device))
-            for t in made:
-                t.record_stream(stream)
+        _behind(stream, made, params.device)   # (filled on the current stream, too)
         v = made.pop() if v is None else v
         k = made.pop() if k is None else k
     _rows("specattn_kv4_read", k, v, codes, params, start, n, block_table, pages_per_seq, status, stream)
@@ -171,6 +184,7 @@ def kv4_verify(q: torch.Tensor, codes: torch.Tensor, params: torch.Tensor, kv_le
     positions (idx [B, n_groups, stride], counts [B, n_groups]; all positions where ``dense``) and the tail of a 4-bit
     cache.  Returns (out [B, T, H_q, 128] of q's type, or float32 where ``out`` is, lse f32 [B, T, H_q], status)."""
     index = _device(q, codes, params, kv_len, block_table, None if dense else idx, None if dense else counts, out, lse, status, workspace)
+    assert dense or (idx is not None and counts is not None), "idx and counts expected, or dense"
     shape = q.shape
     # (out, lse and the workspace are made here or looked at by every call)
     key = (shape, q.dtype, n_groups, dense, sm_scale, tail_len, flags, out is not None and out.dtype is _F32, index,
@@ -221,10 +235,9 @@ def kv4_verify(q: torch.Tensor, codes: torch.Tensor, params: torch.Tensor, kv_le
         a.idx, a.counts = idx.data_ptr(), _ints(counts, rows[0] * n_groups, "counts")
     a.out, a.lse, a.workspace = out.data_ptr(), lse.data_ptr(), workspace.data_ptr()
     a.status = _ints(status, rows[0], "status")
-    _call("specattn_kv4_verify", ref, index, stream)
     if stream is not None:
-        for t in made:
-            t.record_stream(stream)   # allocated here, used on the caller's stream
+        _behind(stream, made, index)
+    _call("specattn_kv4_verify", ref, index, stream)
     return out, lse, status
 
 
@@ -232,10 +245,11 @@ def accumulate_attention(draft_probs: Sequence[torch.Tensor | None], kv_len: tor
                          n_groups: int = 1, head_group: Sequence[int] | None = None, decay: float = 1.0,
                          out: torch.Tensor | None = None, row_status: torch.Tensor | None = None, stream=None):
     """specattn_accumulate: out = decay * scores + the attention that each position got in ``draft_probs`` (per draft
-    layer a float32 tensor [B, H_d, gamma, L_stride], or None to leave the layer's scores alone).  scores, out: float32
+    layer a float32 tensor [B, H_d, gamma, L_stride], or None to leave the layer's entries of out alone).  scores, out: float32
     [n_layers, B, n_groups, L]; out None: in place; scores None: zeros.  Returns (out, row_status)."""
     n = len(draft_probs)
-    probs = next(t for t in draft_probs if t is not None)
+    probs = next((t for t in draft_probs if t is not None), None)
+    assert probs is not None, "draft_probs: a layer's at least"
     if out is None:
         assert scores is not None, "scores or out expected"
         out = scores
@@ -328,10 +342,9 @@ def evict(scores: torch.Tensor, kv_len: torch.Tensor, budget: int, *, n_sink: in
     a.positions = None if positions is None else _like_scores(positions, scores, _I32, "positions")
     a.positions_out = None if positions_out is None else _like_scores(positions_out, scores, _I32, "positions_out")
     a.scores_out = None if scores_out is None else _like_scores(scores_out, scores, _F32, "scores_out")
-    _call("specattn_evict", ref, index, stream)
     if stream is not None:
-        for t in made:
-            t.record_stream(stream)
+        _behind(stream, made, index)
+    _call("specattn_evict", ref, index, stream)
     return src, dst, n_moves, new_len
 
 
@@ -344,7 +357,8 @@ def move_rows(pools: Sequence[torch.Tensor], src: torch.Tensor, dst: torch.Tenso
     n = len(pools)
     if n == 0:
         if status is not None:
-            status.zero_()
+            with torch.cuda.stream(stream):
+                status.zero_()
         return status
     assert params is None or len(params) == n
     index = _device(src, dst, n_moves, block_table, status, *pools, *(params or ()))
@@ -357,6 +371,7 @@ def move_rows(pools: Sequence[torch.Tensor], src: torch.Tensor, dst: torch.Tenso
         n_pages, two, page, heads, width = pool.shape
         b, g, stride = src.shape
         assert two == 2 and pool.stride(4) == 1
+        _apart(pool, *(() if par is None else (par,)))
         a = MoveArgs()
         a.struct_size = C.sizeof(MoveArgs)
         a.n_pools, a.batch, a.n_groups, a.n_kv_heads, a.page_size, a.n_pages = n, b, g, heads, page, n_pages

@@ -256,9 +256,9 @@ int rows_call(const specattn_kv4_rows_args* args, void* cuda_stream, bool append
   // as many tokens to a block as give its half-warps kRows rows each
   int per_block = kHalfWarps * kRows / (2 * A.n_kv_heads);
   // (a few tokens are spread over more blocks: latency is all there is to them)
-  while (per_block > 1 && static_cast<long long>(A.batch) * ((A.n_tokens + per_block - 1) / per_block) < sms) per_block = (per_block + 1) / 2;
+  while (per_block > 1 && static_cast<long long>(A.batch) * (((A.n_tokens - 1) / per_block + 1)) < sms) per_block = (per_block + 1) / 2;
   if (per_block < 1) per_block = 1;
-  const dim3 grid((A.n_tokens + per_block - 1) / per_block, A.batch);
+  const dim3 grid((A.n_tokens - 1) / per_block + 1, A.batch);
   const bool half = A.cache.dtype == SPECATTN_DTYPE_FP16;
   if (append) {
     if (half)

@@ -120,7 +120,14 @@ REFUSALS = [
                              ("q", None, NULL), ("kv_len", None, NULL), ("idx", None, NULL), ("counts", None, NULL), ("out", None, NULL),
                              ("lse", None, NULL), ("workspace", None, NULL), ("q", POINTER + 8, ALIGN), ("out", POINTER + 8, ALIGN),
                              ("workspace", POINTER + 128, ALIGN), ("cache.codes", None, NULL), ("cache.dtype", -1, RANGE),
-                             ("cache.n_pages", 1 << 31, RANGE), ("cache.stride_head", 8, ALIGN)]),
+                             ("cache.n_pages", 1 << 31, RANGE), ("cache.stride_head", 8, ALIGN), ("n_q_heads", 1 << 30, UNSUPPORTED),
+                             ("cache.stride_page", -1024, UNSUPPORTED), ("cache.stride_kv", -1024, UNSUPPORTED),
+                             ("cache.stride_slot", -64, UNSUPPORTED), ("cache.stride_head", -64, UNSUPPORTED),
+                             ("cache.pstride_page", -2, UNSUPPORTED), ("cache.pstride_kv", -2, UNSUPPORTED),
+                             ("cache.pstride_slot", -2, UNSUPPORTED), ("cache.pstride_head", -2, UNSUPPORTED),
+                             ("cache.stride_page", 1 << 36, UNSUPPORTED), ("cache.stride_slot", 1 << 36, UNSUPPORTED),
+                             ("cache.stride_kv", 1 << 36, UNSUPPORTED), ("cache.pstride_page", 1 << 33, UNSUPPORTED),
+                             ("cache.block_table_stride", 1 << 31, UNSUPPORTED)]),
     ("accumulate", _accumulate, [("struct_size", 0, SIZE), ("n_layers", 0, RANGE), ("n_layers", 65, RANGE), ("batch", -1, RANGE), ("gamma", 0, RANGE),
                                  ("gamma", 1025, UNSUPPORTED), ("n_groups", 0, RANGE), ("n_draft_heads", 257, RANGE), ("L_stride", 0, RANGE),
                                  ("L_stride", 196612, RANGE), ("L_stride", 63, ALIGN), ("score_stride", 0, RANGE), ("decay", -0.5, RANGE),
@@ -137,7 +144,9 @@ REFUSALS = [
                           ("param_bytes", 4, NULL), ("params", (C.c_void_p * 1)(POINTER), NULL), ("pools", None, NULL),
                           ("pools", (C.c_void_p * 1)(None), NULL), ("pools", (C.c_void_p * 1)(POINTER + 8), ALIGN), ("src", None, NULL),
                           ("dst", None, NULL), ("n_moves", None, NULL), ("block_table_stride", -1, RANGE), ("move_stride", -1, RANGE),
-                          ("batch", 70000, UNSUPPORTED)]),
+                          ("batch", 70000, UNSUPPORTED), ("stride_page", -16, RANGE), ("stride_kv", -16, RANGE), ("stride_slot", -16, RANGE),
+                          ("stride_head", -16, RANGE), ("pstride_page", -4, RANGE), ("pstride_kv", -4, RANGE),
+                          ("pstride_slot", -4, RANGE), ("pstride_head", -4, RANGE)]),
 ]
 
 
@@ -235,6 +244,21 @@ def test_types_and_shapes_that_are_refused(recorder):
         sa.accumulate_attention([torch.zeros(2, 1, 1, 8)], n, torch.zeros(2, 2, 1, 8))
     with pytest.raises(AssertionError):
         sa.accumulate_attention([torch.zeros(2, 1, 1, 8)], n)
+    with pytest.raises(AssertionError):
+        sa.accumulate_attention([None, None], n, torch.zeros(2, 2, 1, 8))
+    with pytest.raises(AssertionError):
+        sa.kv4_verify(q, codes, params, n, block_table=table, idx=idx)
+    # what is written twice in one place
+    same = k[:, :1].expand(2, 3, 2, 128)
+    append(k=same, v=same, block_table=table)
+    for bad in (dict(k=same), dict(v=same)):
+        with pytest.raises(AssertionError):
+            sa.kv4_read(codes, params, n, block_table=table, **({"k": k, "v": k} | bad))
+    with pytest.raises(AssertionError):
+        append(codes=codes[:1].expand(4, 2, 16, 2, 64), block_table=table)
+    moves = torch.zeros(2, 1, 8, dtype=torch.int32)
+    with pytest.raises(AssertionError):
+        sa.move_rows([codes[:, :1].expand(4, 2, 16, 2, 64)], moves, moves, cnt, block_table=table)
 
 
 def test_kept_structs_follow_every_value_of_a_call(recorder):
