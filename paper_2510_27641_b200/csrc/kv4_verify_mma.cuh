@@ -352,7 +352,7 @@ __device__ __forceinline__ void mma_path(const Kv4Params& P, const Partition& pa
     __syncthreads();  // the records have been read
     at = u_start + seg1;
     if (seg1 == n_chunks) {
-      u_start += n_chunks;
+      at = u_start += n_chunks + part.between;
       do {
         ++u;
       } while (u < units.n && at < last && chunks_of(P, u, kChunk) == 0);

@@ -455,7 +455,7 @@ __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& par
     const bool first_part = seg0 == 0, whole = seg0 == 0 && seg1 == n_tiles;
     at = u_start + seg1;
     if (seg1 == n_tiles) {
-      u_start += n_tiles;
+      at = u_start += n_tiles + part.between;
       do {
         ++u;
       } while (u < units.n && at < last && chunks_of(P, u, kTile) == 0);
