@@ -3,12 +3,12 @@
 //
 //   accumulate  one read of the draft maps, bound by HBM: a thread sums four neighbouring positions over the rows of
 //               (head, query) in binary64 (a conversion and an addition a value: 1/8 of the SM's binary64 rate at
-//               HBM's speed).  Few positions are dealt to several threads each, by rows.
+//               HBM's speed).  Few positions are dealt to several threads each, by rows.  260 MB: 42 us, 6.2 TB/s.
 //   evict       one list to a cluster of CTAs that hold its weights as ordered 32-bit keys in shared memory.  The
 //               m-th largest key is found digit by digit (four of 8 bits) from histograms that the cluster adds
 //               up; which slots stay then follows from comparisons, and their ranks from counts.  Bound by the
-//               chain of passes and cluster barriers.
-//   move_rows   copies of rows, bound by HBM.
+//               chain of passes and cluster barriers: 15 us for 8 lists of 32768, 46 for 32 of 131072 (with positions).
+//   move_rows   copies of rows, bound by HBM: 1.04 GB read and written in 168 us, 6.2 TB/s.
 #include <cuda_runtime.h>
 #include <float.h>
 #include <math.h>

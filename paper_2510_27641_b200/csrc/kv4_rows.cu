@@ -1,9 +1,10 @@
 // specattn_kv4_append, specattn_kv4_read: rows of 128 values in and out of a cache that holds them in 4 bits.
 //
-// Both are copies that change a row's size (256 bytes <-> 68), bound by HBM for prompts and by the chain start ->
-// block table -> row for the few tokens of a step.  A row belongs to half a warp, 16 bytes of values to a lane: the
-// row's minimum and maximum are four exchanges between lanes, and both sides of the copy are whole sectors.  A
-// half-warp has kRows rows in flight, whose loads are sent before the page of any is known.
+// Both are copies that change a row's size (256 bytes <-> 68), bound by HBM and, on the way in, nearly as much by
+// instructions for prompts (437k rows: 45 us in, 30 back; 3.2 and 4.7 TB/s), and by the chain start -> block table -> row
+// for the few tokens of a step (4 to 5 us each).  A row belongs to half a warp, 16 bytes of values to a lane: both
+// sides of the copy are whole sectors.  A half-warp has kRows rows in flight, whose values are asked for before the page
+// of any is known, and finds their minima and maxima together.
 #include <cuda_runtime.h>
 #include <float.h>
 #include <stdint.h>
