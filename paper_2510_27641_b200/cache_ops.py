@@ -52,7 +52,7 @@ def _strides(t: torch.Tensor, first: int, last: int):
 def _behind(stream, made, device):
     """What was allocated on the current stream is used on the caller's: whoever had the memory before is done by then, and
     nobody gets it earlier than that stream is done."""
-    if stream is not None and made:
+    if made and stream != torch.cuda.current_stream(device):
         stream.wait_stream(torch.cuda.current_stream(device))
         for t in made:
             t.record_stream(stream)
@@ -155,7 +155,8 @@ def kv4_read(codes: torch.Tensor, params: torch.Tensor, start: torch.Tensor, *, 
     if k is None or v is None:
         shape = (start.shape[0], int(n_tokens), codes.shape[3], 128) if k is None and v is None else (v if k is None else k).shape
         made = [torch.zeros(shape, dtype=params.dtype, device=params.device) for x in (k, v) if x is None]
-        _behind(stream, made, params.device)   # (filled on the current stream, too)
+        if stream is not None:
+            _behind(stream, made, params.device)   # (filled on the current stream, too)
         v = made.pop() if v is None else v
         k = made.pop() if k is None else k
     _rows("specattn_kv4_read", k, v, codes, params, start, n, block_table, pages_per_seq, status, stream)

@@ -132,6 +132,9 @@ EVICT_CASES = [
     (1, 2, 1, 196608, [196608, 300000], 100001, 0, 64),      # a length beyond the row is clamped
     (3, 40, 3, 2100, [2100 - 7 * b for b in range(40)], 1900, 2, 30),   # more lists than CTAs at once
     (1, 310, 1, 3000, [3000] * 310, 1500, 0, 0),
+    (1, 8, 1, 32768, [32768 - 5000 * b for b in range(6)] + [3, 0], 16384, 4, 64),      # eight CTAs to a list
+    (1, 75, 2, 17001, [17001 - 200 * b for b in range(75)], 9000, 4, 64),               # two, of more CTAs than SMs
+    (1, 20, 1, 16385, [16385, 8193] * 10, 8192, 0, 100),                                # slices of 8192 and more, 1024 threads
 ]
 
 

@@ -262,6 +262,67 @@ def test_long_lists_split_over_the_gpu(T, Hq, Hkv, lens, counts):
         _check(c, out, lse)
 
 
+@pytest.mark.parametrize("T,Hq,Hkv,G", [(1, 8, 8, 8), (5, 32, 8, 1), (5, 64, 8, 8), (8, 64, 8, 1)])
+def test_many_units_of_very_different_lengths(T, Hq, Hkv, G):
+    """More units than CTAs, from one position to thousands, some empty: a CTA's run may end in front of a unit's first chunk."""
+    lens = [(1, 5000, 33, 700, 0, 64, 2500)[b % 7] + b % 5 for b in range(41)]
+    counts = [0 if n < 2 else n - 1 - b % 2 for b, n in enumerate(lens)]
+    c = _case(46, len(lens), T, Hq, Hkv, lens, counts, G=G, tail=T - 1, page=24)
+    few = [0, 1, 3, 4, 5, 18, 40]
+    pick = lambda t: t if t is None else t[few]
+    sub = dict(c, q=c["q"][few], table=pick(c["table"]), lens=[lens[b] for b in few], lists=[c["lists"][b] for b in few])
+    for engine in _engines(T, Hq, Hkv):
+        status = torch.full((len(lens),), 7, dtype=torch.int32, device=DEV)
+        out, lse, _ = _run(c, engine, status=status)
+        assert not status.any()
+        _check(sub, out[few], lse[few])
+
+
+def test_a_context_beyond_the_largest_table():
+    """2^23 positions, the most that a table may hold: one more is reported."""
+    sa = _sa()
+    codes, params = sa.kv4_cache(1, 64, 1)
+    x = torch.randn(1, 64, 1, 128, generator=_gen(48)).to(torch.bfloat16).to(DEV)
+    table = torch.zeros(1, 1 << 17, dtype=torch.int32, device=DEV)
+    sa.kv4_append(x, x, codes, params, torch.zeros(1, dtype=torch.int32, device=DEV), block_table=table)
+    q = torch.randn(1, 1, 2, 128, generator=_gen(49)).to(torch.bfloat16).to(DEV)
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    got = []
+    for n in (64, 1 << 23, (1 << 23) + 1, 2 ** 31 - 1):
+        out, lse, _ = sa.kv4_verify(q, codes, params, torch.tensor([n], dtype=torch.int32, device=DEV), block_table=table, dense=True, status=status)
+        got.append((out.float(), lse, status.item()))
+    assert [s for _, _, s in got] == [0, 0, sa.ROW_BAD_INDEX, sa.ROW_BAD_INDEX]
+    # the same 64 rows 2^17 times over: the output stays (two roundings of half a step of bf16), the sum of weights grows with their
+    # number (a thread adds a few hundred to a few thousand of them, 2^-24 each time: 2^-12 at worst, and the joins)
+    assert float((got[1][0] - got[0][0]).abs().max()) <= 2.0 ** -7 * float(got[0][0].abs().max())
+    assert float((got[1][1] - got[0][1] - 17 * math.log(2)).abs().max()) <= 1e-3
+
+
+def test_memory_that_the_current_stream_still_uses_is_waited_for():
+    """What a call on another stream allocates may be memory that work on the current stream has yet to write."""
+    sa = _sa()
+    c = _case(98, 2, 6, 32, 8, [300, 200], [250, 100])
+    up = lambda t: t.to(DEV)
+    q, codes, params, table, idx, counts = up(c["q"]), _to_gpu(c["codes"]), _to_gpu(c["params"]), up(c["table"]), up(c["idx"]), up(c["counts"])
+    lens = torch.tensor(c["lens"], dtype=torch.int32, device=DEV)
+    kw = dict(block_table=table, idx=idx, counts=counts)
+    ref = sa.kv4_verify(q, codes, params, lens, **kw)
+    start = torch.zeros(2, dtype=torch.int32, device=DEV)
+    ref_k, ref_v, _ = sa.kv4_read(codes, params, start, n_tokens=200, block_table=table)
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        late = [torch.empty_like(t) for t in (ref[0], ref[1], ref_k, ref_v)]
+        torch.cuda._sleep(20_000_000)
+        for t in late:
+            t.fill_(float("nan"))
+        del late, t
+        out, lse, _ = sa.kv4_verify(q, codes, params, lens, stream=stream, **kw)
+        k, v, _ = sa.kv4_read(codes, params, start, n_tokens=200, block_table=table, stream=stream)
+        torch.cuda.synchronize()
+        assert torch.equal(out, ref[0]) and torch.equal(lse, ref[1]) and torch.equal(k, ref_k) and torch.equal(v, ref_v)
+
+
 def test_calls_long_enough_for_tcgen05_take_it_by_themselves():
     c = _case(44, 2, 6, 12, 2, [150000, 100000], None, dense=True)
     out, lse, _ = _run(c)
