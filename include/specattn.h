@@ -460,7 +460,8 @@ typedef struct specattn_kv4_cache {
  * [0, n_tokens] are clamped).  status (int32 [batch], optional) is cleared by the call and receives
  * SPECATTN_ROW_BAD_INDEX where a position is negative or beyond the block table or its page id out of range
  * (that row is skipped) and, on append, SPECATTN_ROW_INVALID_VALUE.  No two rows of a call may be written to one
- * place (a page in two sequences' tables, overlapping k or v of a read).  head_dim == 128. */
+ * place (a page in two sequences' tables, overlapping k or v of a read).
+ * Requirements: head_dim == 128; batch and n_kv_heads at most 65535. */
 typedef struct specattn_kv4_rows_args {
   uint32_t struct_size;
   int32_t batch;
@@ -557,7 +558,8 @@ int specattn_kv4_verify(const specattn_kv4_verify_args* args, void* cuda_stream)
  * scores_out.  Other entries are left as they were.  Where a contributing probability is negative,
  * NaN or infinite the position gets its old value, undecayed, and row_status[u,b,g] (optional, cleared by
  * the call, for every u) SPECATTN_ROW_INVALID_PROB.
- * Arrays, limits and alignment of draft_probs, kv_len and head_group as in specattn_select_topp;
+ * Arrays, limits and alignment of draft_probs, kv_len and head_group as in specattn_select_topp (gamma at most
+ * SPECATTN_MAX_ROWS_PER_LIST, batch and, where heads are grouped, batch * n_groups at most 65535);
  * scores are binary32 [n_layers, batch, n_groups, score_stride]. */
 typedef struct specattn_accumulate_args {
   uint32_t struct_size;
@@ -595,7 +597,7 @@ int specattn_accumulate(const specattn_accumulate_args* args, void* cuda_stream)
  *   >= m left as they were; may equal positions.
  * All of scores, positions, scores_out and positions_out are [n_layers, batch, n_groups, L].
  * Requirements: 1 <= L <= SPECATTN_MAX_KV_LEN; budget >= 1; n_sink, n_recent >= 0, their sum <= budget;
- * move_stride >= min(budget, L - budget); new_len must not be kv_len or seq_len. */
+ * move_stride >= min(budget, L - budget); n_layers * batch * n_groups <= 2^24; new_len must not be kv_len or seq_len. */
 typedef struct specattn_evict_args {
   uint32_t struct_size;
   int32_t n_layers;
@@ -631,7 +633,8 @@ int specattn_evict(const specattn_evict_args* args, void* cuda_stream);
  * them, 4-byte aligned.  No position may be both a source and a destination of a list, nor twice a destination; and no
  * page that a move reads or writes may be in two sequences' tables (a shared prefix has to be copied first).
  * status (int32 [batch], optional) is cleared by the call and receives SPECATTN_ROW_BAD_INDEX where a
- * position is negative or beyond the block table, or its page id outside [0, n_pages) (the move is skipped). */
+ * position is negative or beyond the block table, or its page id outside [0, n_pages) (the move is skipped).
+ * Requirements: row_bytes 16 to 4096, param_bytes up to 256, n_kv_heads up to 1024, batch * n_groups up to 65535. */
 typedef struct specattn_move_args {
   uint32_t struct_size;
   int32_t n_pools;
