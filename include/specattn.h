@@ -455,7 +455,7 @@ typedef struct specattn_kv4_cache {
  * specattn_kv4_read   -- the reverse: rows start[b] + t, t < n_new[b], as 16-bit values
  * (s c + z in binary32, rounded to even).  Rows t >= n_new[b] of the buffers are neither read nor
  * written by either.
- * k, v: element (b, t, head, e) at b*stride_batch + t*stride_token + head*stride_head + e, 16-byte
+ * k, v (not looked at where n_tokens == 0): element (b, t, head, e) at b*stride_batch + t*stride_token + head*stride_head + e, 16-byte
  * aligned, strides multiples of 8.  n_new == NULL: n_tokens of every sequence (values beyond
  * [0, n_tokens] are clamped).  status (int32 [batch], optional) is cleared by the call and receives
  * SPECATTN_ROW_BAD_INDEX where a position is negative or beyond the block table or its page id out of range
@@ -527,7 +527,7 @@ typedef struct specattn_kv4_verify_args {
   specattn_kv4_cache cache;
   const void* q;
   const int32_t* kv_len; /* [batch] */
-  const int32_t* idx;    /* [batch, n_groups, idx_stride] */
+  const int32_t* idx;    /* [batch, n_groups, idx_stride]; may be NULL where idx_stride == 0 (the tail alone) */
   int64_t idx_stride;
   const int32_t* counts; /* [batch, n_groups] */
   float sm_scale;        /* > 0, or 0 => 1/sqrt(head_dim); negative or NaN is rejected */

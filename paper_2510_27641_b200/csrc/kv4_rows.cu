@@ -221,7 +221,7 @@ int rows_call(const specattn_kv4_rows_args* args, void* cuda_stream, bool append
   if (A.head_dim != kKv4D) return SPECATTN_ERR_UNSUPPORTED;
   const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
   if (A.batch == 0) return SPECATTN_OK;
-  if (!A.k || !A.v || !A.start) return SPECATTN_ERR_NULL;
+  if ((A.n_tokens > 0 && (!A.k || !A.v)) || !A.start) return SPECATTN_ERR_NULL;
   const int cb = kv4_check_buffers(A.cache);
   if (cb != SPECATTN_OK) return cb;
   if (reinterpret_cast<uintptr_t>(A.k) % 16 != 0 || reinterpret_cast<uintptr_t>(A.v) % 16 != 0) return SPECATTN_ERR_ALIGN;

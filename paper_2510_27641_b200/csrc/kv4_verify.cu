@@ -244,8 +244,8 @@ extern "C" int specattn_kv4_verify(const specattn_kv4_verify_args* args, void* c
   const specattn_kv4_verify_args& A = *args;
   if (A.batch == 0) return SPECATTN_OK;
   if (!A.q || !A.kv_len || !A.out || !A.lse || !A.workspace) return SPECATTN_ERR_NULL;
-  if (!A.dense && (!A.idx || !A.counts)) return SPECATTN_ERR_NULL;
   if (!A.dense && A.idx_stride < 0) return SPECATTN_ERR_RANGE;
+  if (!A.dense && ((A.idx_stride > 0 && !A.idx) || !A.counts)) return SPECATTN_ERR_NULL;
   if ((!A.dense && A.idx_stride > kMaxPositions) ||
       (A.dense && A.cache.block_table_stride > kMaxPositions / A.cache.page_size))
     return SPECATTN_ERR_UNSUPPORTED;

@@ -172,6 +172,14 @@ def test_nothing_to_do_and_no_arguments(name, make):
     a = make()
     a.batch = 0
     assert entry(C.byref(a), None) == 0
+    if name in ("kv4_append", "kv4_read"):   # no token: no rows to look at
+        a = make()
+        a.n_tokens, a.k, a.v, a.status = 0, None, None, None
+        assert entry(C.byref(a), None) == 0
+    if name == "move_rows":
+        a = make()
+        a.move_stride, a.src, a.dst, a.status = 0, None, None, None
+        assert entry(C.byref(a), None) == 0
 
 
 def test_tensors_that_no_call_takes():

@@ -278,6 +278,28 @@ def test_many_units_of_very_different_lengths(T, Hq, Hkv, G):
         _check(sub, out[few], lse[few])
 
 
+@pytest.mark.parametrize("T,Hq,Hkv", [(3, 16, 4), (5, 64, 8)])
+def test_no_rows_and_lists_without_room(T, Hq, Hkv):
+    """No tokens to write or read; lists of no room, so that the tail is all there is, or nothing is."""
+    sa = _sa()
+    c = _case(50, 2, T, Hq, Hkv, [40, 0], [0, 0], tail=T)
+    codes, params, table = _to_gpu(c["codes"]), _to_gpu(c["params"]), c["table"].to(DEV)
+    none = torch.empty(2, 0, Hkv, 128, dtype=torch.bfloat16, device=DEV)
+    start, status = torch.zeros(2, dtype=torch.int32, device=DEV), torch.full((2,), 9, dtype=torch.int32, device=DEV)
+    before = codes.clone()
+    sa.kv4_append(none, none, codes, params, start, block_table=table, status=status)
+    assert torch.equal(codes, before) and not status.any()
+    k, v, _ = sa.kv4_read(codes, params, start, n_tokens=0, block_table=table, status=status)
+    assert k.shape == v.shape == (2, 0, Hkv, 128)
+    idx, counts = torch.empty(2, 1, 0, dtype=torch.int32, device=DEV), torch.zeros(2, 1, dtype=torch.int32, device=DEV)
+    lens = torch.tensor(c["lens"], dtype=torch.int32, device=DEV)
+    kw = dict(block_table=table, idx=idx, counts=counts, status=status)
+    out, lse, _ = sa.kv4_verify(c["q"].to(DEV), codes, params, lens, tail_len=T, **kw)
+    _check(c, out, lse)
+    out, lse, _ = sa.kv4_verify(c["q"].to(DEV), codes, params, lens, **kw)
+    assert not out.any() and torch.all(lse == float("-inf")) and not status.any()
+
+
 def test_a_context_beyond_the_largest_table():
     """2^23 positions, the most that a table may hold: one more is reported."""
     sa = _sa()
