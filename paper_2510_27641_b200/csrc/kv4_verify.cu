@@ -38,7 +38,7 @@ namespace {
 // from 33 rows on.  There tcgen05 takes 33 to 40 rows, from kTensorLeast chunks of 32 positions to an SM on that the call's
 // sizes (idx_stride, or the block table) leave room for: 8 sequences x 8 heads x 32768 positions with 40 rows are 159 us
 // against 225, x 2400 (33 chunks) 29.1 against 29.9, x 1200 23.7 against 21.0.  Fewer rows run as fast or faster on
-// mma.sync (24 / 32 rows over 32768: 127 / 152 against 139 / 148; over 2400: 21.9 / 25.5 against 25.4 / 26.9), and with more the
+// mma.sync (24 / 32 rows over 32768: 122 / 150 against 139 / 148; over 2400: 21.9 / 25.5 against 25.4 / 26.9), and with more the
 // sums of tcgen05's threads do not fit their registers (48 rows: 226 against 234).  A kernel for each path: one for both, choosing by
 // the lengths it found, cost small calls 3 us and 10 to 17 where the instructions were not in L2.
 constexpr int kTensorLeast = 32;
@@ -48,7 +48,10 @@ struct Config {
   static constexpr int kTiles = (R8 + kGroups - 1) / kGroups;  // of eight queries
   static constexpr bool kTensor = R8 == 5;
   static constexpr int kWarps = R8 == 1 ? 16 : R8 == 2 ? 12 : 8;
-  static constexpr int kStages = R8 <= 2 ? 3 : 4;
+  // Two chunks of 32 positions to a warp: one under way, one at work.  What the ring leaves is L1, where lists, tables and the
+  // sectors of (s, z) pairs are met again (against three or four: 20 rows over 32 ragged lists 84 against 90 us, 4 rows over 16
+  // ragged contexts 49 against 53, 24 rows over 8 x 32768 122 against 125).
+  static constexpr int kStages = 2;
   using Mma = MmaPath<kTiles, kWarps, kStages>;
 };
 
