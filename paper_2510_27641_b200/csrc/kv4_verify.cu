@@ -36,9 +36,9 @@ namespace {
 //
 // mma.sync: as many warps as hold a warp's output in registers.  Two groups of query rows, which read a unit's rows twice,
 // from 33 rows on.  There tcgen05 takes 33 to 40 rows, from kTensorLeast chunks of 32 positions to an SM on that the call's
-// sizes (idx_stride, or the block table) leave room for: 8 sequences x 8 heads x 32768 positions with 40 rows are 159 us
-// against 225, x 2400 (33 chunks) 29.1 against 29.9, x 1200 23.7 against 21.0.  Fewer rows run as fast or faster on
-// mma.sync (24 / 32 rows over 32768: 122 / 150 against 139 / 148; over 2400: 21.9 / 25.5 against 25.4 / 26.9), and with more the
+// sizes (idx_stride, or the block table) leave room for: 8 sequences x 8 heads x 32768 positions with 40 rows are 155 us
+// against 227, x 2400 (33 chunks) 29.1 against 29.9, x 1200 23.7 against 21.0.  Fewer rows run as fast or faster on
+// mma.sync (24 / 32 rows over 32768: 122 / 147 against 139 / 148; over 2400: 21.5 / 25.5 against 25.4 / 26.9), and with more the
 // sums of tcgen05's threads do not fit their registers (48 rows: 226 against 234).  A kernel for each path: one for both, choosing by
 // the lengths it found, cost small calls 3 us and 10 to 17 where the instructions were not in L2.
 constexpr int kTensorLeast = 32;

@@ -17,7 +17,7 @@
 // its own, and run a phase apart.  In a group's turn:
 //     scores of tile i from tensor memory | K of tile i + 1 into it | vote (may the maximum stay?) and S^T of i + 1 starts |
 //     V of tile i, copies of tile i + 3 asked for | weights of tile i | O^T of tile i starts
-// 40 rows over 8 x 8 x 32768 positions: 159 us, 1.8 TB/s.  A tile takes an SM about 2700 cycles, where HBM would take 757 and
+// 40 rows over 8 x 8 x 32768 positions: 155 us, 1.9 TB/s.  A tile takes an SM about 2600 cycles, where HBM would take 757 and
 // shared memory (16 KB of copies written and read, 32 KB of V operand, W and Q) 940: what bounds it is the chain of
 // instructions, barriers and products in flight in a group's turn.  (Taking 8 off by one more product with a constant
 // operand instead: 137 to 141 us at 24 rows.)
