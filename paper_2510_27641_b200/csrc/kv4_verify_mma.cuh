@@ -248,7 +248,7 @@ __device__ __forceinline__ void mma_path(const Kv4Params& P, const Partition& pa
               v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 16));
               // (a query that sees nothing of the warp's first tile sees nothing of the later ones)
               const float d = begins ? (v == -INFINITY ? 0.f : v) : fmaxf(v, 0.f);
-              f[e] = ex2(-d);
+              f[e] = begins ? 0.f : ex2(-d);  // (the sums are still 0, and the first maximum may be far below it: no 0 inf)
               down[e] = d;
               s[nt][e] -= d, s[nt][2 + e] -= d;
             }
@@ -256,7 +256,7 @@ __device__ __forceinline__ void mma_path(const Kv4Params& P, const Partition& pa
             l[nt] = mul2(l[nt], two(f[0], f[1]));
             y[nt] = mul2(y[nt], two(f[0], f[1]));
 #pragma unroll
-            for (int e = 0; e < 2; ++e) f[e] = begins ? 0.f : f[e] * scale_now;
+            for (int e = 0; e < 2; ++e) f[e] *= scale_now;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               acc8[nt][e] *= f[e & 1];

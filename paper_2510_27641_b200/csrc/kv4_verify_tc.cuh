@@ -375,7 +375,7 @@ __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& par
             const float v = fmaxf(fmaxf(S.red[g][0][r][0], S.red[g][1][r][0]), fmaxf(S.red[g][2][r][0], S.red[g][3][r][0]));
             // (a query that sees nothing of the group's first tile sees nothing of the later ones)
             const float d = i == 0 ? (v == -INFINITY ? 0.f : v) : fmaxf(v, 0.f);
-            f[e] = ex2(-d);
+            f[e] = i == 0 ? 0.f : ex2(-d);  // (the sums are still 0, and the first maximum may be far below it: no 0 inf)
             x[c + e] -= d;
             o[e] *= f[e] * scale_now;
             down[e] = d;
