@@ -468,8 +468,10 @@ __global__ void __launch_bounds__(kMoveThreads) move_rows_kernel(const __grid_co
   __shared__ longlong2 row[kMoveMost], word[kMoveMost];  // offsets of source and destination; source -1: not to be moved
   const int b = blockIdx.y / P.G, g = blockIdx.y - b * P.G;
   const long long j0 = static_cast<long long>(blockIdx.x) * P.per_block;
-  const int n = static_cast<int>(min(static_cast<long long>(P.per_block), min(static_cast<long long>(P.n_moves[blockIdx.y]), P.move_stride) - j0));
-  if (n <= 0) return;
+  // (compared in 64 bits: a count near -2^31 less j0 would come out positive in 32, and row[] would be overrun)
+  const long long left = min(static_cast<long long>(P.n_moves[blockIdx.y]), P.move_stride) - j0;
+  if (left <= 0) return;
+  const int n = static_cast<int>(min(left, static_cast<long long>(P.per_block)));
   const long long first = static_cast<long long>(blockIdx.y) * P.move_stride + j0;
   const int group = P.G > 1 ? g : 0;
   for (int j = threadIdx.x; j < n; j += kMoveThreads) {
