@@ -500,7 +500,7 @@ int specattn_kv4_read(const specattn_kv4_rows_args* args, void* cuda_stream);
  * Positions whose row holds NaN make the rows that attend them NaN; rows that no list names, masked tail rows
  * and the rest of the last page are not looked at.  Values are summed before the division by sum p_i: their magnitude
  * times the number of positions has to stay within binary32.  A weight's product with its row's scale keeps its 11 bits while
- * it is at least 2^-19 of the largest scale of the rows that the query has met.
+ * it is at least 2^-19 of the largest scale of the rows that the query has met, and at least 2^-141.
  * out must not overlap q.
  * Requirements: head_dim == 128; n_q * (n_q_heads / n_kv_heads) <= 64; batch * n_kv_heads <= 2048; lists
  * and, where dense, block_table_stride * page_size of at most 2^23 positions; and (SPECATTN_ERR_UNSUPPORTED otherwise)

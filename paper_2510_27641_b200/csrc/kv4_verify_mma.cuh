@@ -232,9 +232,9 @@ __device__ __forceinline__ void mma_path(const Kv4Params& P, const Partition& pa
           t_max = t_max <= FLT_MAX ? t_max : 0.f;
 #pragma unroll
           for (int o = 16; o > 0; o >>= 1) t_max = fmaxf(t_max, __shfl_xor_sync(0xffffffffu, t_max, o));
-          // t_max up in [32, 64)
+          // t_max up in [32, 64), or up = 2^127, the largest power of two
           float up_now = up;
-          if (t_max > 0.f) up_now = fminf(up, __int_as_float((127 + min(5 + 127 - (__float_as_int(t_max) >> 23), 100)) << 23));
+          if (t_max > 0.f) up_now = fminf(up, __int_as_float((127 + min(5 + 127 - (__float_as_int(t_max) >> 23), 127)) << 23));
           const float scale_now = up_now / up;
           up = up_now;
 #pragma unroll

@@ -355,7 +355,7 @@ __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& par
         named_bar_sync(1 + g, 256);
         t_max = fmaxf(fmaxf(S.t_red[g][0], S.t_red[g][1]), fmaxf(S.t_red[g][2], S.t_red[g][3]));
         float up_now = up;
-        if (t_max > 0.f) up_now = fminf(up, __int_as_float((127 + min(5 + 127 - (__float_as_int(t_max) >> 23), 100)) << 23));
+        if (t_max > 0.f) up_now = fminf(up, __int_as_float((127 + min(5 + 127 - (__float_as_int(t_max) >> 23), 127)) << 23));
         const float scale_now = up_now / up;
         up = up_now;
         if (i > 0) {  // the output so far is complete, and has to shrink, too
