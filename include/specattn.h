@@ -491,7 +491,7 @@ int specattn_kv4_read(const specattn_kv4_rows_args* args, void* cuda_stream);
  *   lse   = max s + ln sum_i p_i.
  * An empty list gives out = 0, lse = -inf.  Lists, dense, kv_len, tail_len, sm_scale and n_groups as
  * in specattn_sparse_verify; one query and no list (n_q = 1, dense = 1) is plain decoding.  Scores,
- * sums and outputs are binary32; the weights p_i enter the second product in 11 bits.
+ * sums and outputs are binary32; a weight p_i s_V[i] enters the second product as two 11-bit numbers, 21 bits in all.
  * q is of the cache's dtype, [batch, n_q, n_q_heads, 128], 16-byte aligned; out has the same shape, in
  * that dtype or (out_f32 != 0) binary32, 16-byte aligned; lse binary32 [batch, n_q, n_q_heads].
  * status (int32 [batch], optional) is written by the call: SPECATTN_ROW_BAD_INDEX where a listed
@@ -499,8 +499,9 @@ int specattn_kv4_read(const specattn_kv4_rows_args* args, void* cuda_stream);
  * (such entries are read from position 0 / page 0 instead), else 0.
  * Positions whose row holds NaN make the rows that attend them NaN; rows that no list names, masked tail rows
  * and the rest of the last page are not looked at.  Values are summed before the division by sum p_i: their magnitude
- * times the number of positions has to stay within binary32.  A weight's product with its row's scale keeps its 11 bits while
- * it is at least 2^-19 of the largest scale of the rows that the query has met, and at least 2^-141.
+ * times the number of positions has to stay within binary32.  Such a weight is off
+ * by at most 2^-21 of itself or 2^-29 of the largest scale of the rows that the query has met, whichever is more (scales below 2^-122
+ * count as 2^-122 there).
  * out must not overlap q.
  * Requirements: head_dim == 128; n_q * (n_q_heads / n_kv_heads) <= 64; batch * n_kv_heads <= 2048; lists
  * and, where dense, block_table_stride * page_size of at most 2^23 positions; and (SPECATTN_ERR_UNSUPPORTED otherwise)

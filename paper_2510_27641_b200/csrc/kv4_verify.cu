@@ -8,8 +8,10 @@
 // with 0x000f000f or 0x00f000f0 gives a register of two exact fp16 values and no conversion takes place (five
 // instructions for eight codes; tensor cores take subnormals as they are).  Queries are scaled by a power of two so
 // that they fit fp16 with all of their bits, those that meet the high codes of a byte by 2^-4 more.
-// The second product is taken about the middle of the codes: the weights w = p t are rounded to fp16, and an error of w
-// should be multiplied by a code's distance from 8, not by the code (2 to 3 times the error of the output).
+// fp16 holds 11 bits of a weight w = p t, and sums of outputs in binary32 should not depend on so few: a weight goes in as
+// two fp16 numbers, 21 bits, and the second product runs over both.  (With 11 bits alone 24 rows over 8 x 32768 took 122 us instead
+// of 138, 40 rows 155 instead of 172; the outputs were off by 1e-4 of their scale, fp16 ones by half as much again as their own
+// rounding.)
 //
 // Two paths compute this: on mma.sync (kv4_verify_mma.cuh) and, for 33 to 40 query rows, on tcgen05 (kv4_verify_tc.cuh).
 // Units (sequence, KV head) are cut on the device, where the lengths are; the parts meet through the workspace in a second
@@ -36,21 +38,20 @@ namespace {
 //
 // mma.sync: as many warps as hold a warp's output in registers.  Two groups of query rows, which read a unit's rows twice,
 // from 33 rows on.  There tcgen05 takes 33 to 40 rows, from kTensorLeast chunks of 32 positions to an SM on that the call's
-// sizes (idx_stride, or the block table) leave room for: 8 sequences x 8 heads x 32768 positions with 40 rows are 155 us
-// against 227, x 2400 (33 chunks) 29.1 against 29.9, x 1200 23.7 against 21.0.  Fewer rows run as fast or faster on
-// mma.sync (24 / 32 rows over 32768: 122 / 147 against 139 / 148; over 2400: 21.5 / 25.5 against 25.4 / 26.9), and with more the
-// sums of tcgen05's threads do not fit their registers (48 rows: 226 against 234).  A kernel for each path: one for both, choosing by
+// sizes (idx_stride, or the block table) leave room for: 8 sequences x 8 heads x 32768 positions with 40 rows are 172 us
+// against 260, x 2400 (33 chunks) 31.1 against 33.3, x 1200 25.0 against 22.9.  A kernel for each path: one for both, choosing by
 // the lengths it found, cost small calls 3 us and 10 to 17 where the instructions were not in L2.
 constexpr int kTensorLeast = 32;
-template <int R8>
+template <int R8>  // (0: up to four rows)
 struct Config {
+  static constexpr bool kSpare = R8 == 0;
   static constexpr int kGroups = R8 > 4 ? 2 : 1;               // of query rows, on mma.sync: 32 are as many as registers hold
-  static constexpr int kTiles = (R8 + kGroups - 1) / kGroups;  // of eight queries
+  static constexpr int kTiles = kSpare ? 1 : (R8 + kGroups - 1) / kGroups;  // of eight queries
   static constexpr bool kTensor = R8 == 5;
-  static constexpr int kWarps = R8 == 1 ? 16 : R8 == 2 ? 12 : 8;
+  static constexpr int kWarps = R8 <= 1 ? 16 : R8 == 2 ? 12 : 8;
   // Two chunks of 32 positions to a warp: one under way, one at work.  What the ring leaves is L1, where lists, tables and the
-  // sectors of (s, z) pairs are met again (against three or four: 20 rows over 32 ragged lists 84 against 90 us, 4 rows over 16
-  // ragged contexts 49 against 53, 24 rows over 8 x 32768 122 against 125).
+  // sectors of (s, z) pairs are met again (against three or four, with weights of 11 bits: 20 rows over 32 ragged lists 84
+  // against 90 us, 4 rows over 16 ragged contexts 49 against 53, 24 rows over 8 x 32768 122 against 125).
   static constexpr int kStages = 2;
   using Mma = MmaPath<kTiles, kWarps, kStages>;
 };
@@ -64,7 +65,7 @@ __global__ void __launch_bounds__(Config<R8>::kWarps * 32, 1) kv4_verify_mma_ker
   pdl_wait();  // everything below reads what earlier kernels may have written
   if (threadIdx.x < 2) sh.bad[threadIdx.x] = sh.qmax[threadIdx.x] = 0;
   const Partition part = cut<C::kWarps * 32>(P, kChunk, C::kWarps, 32, ps);
-  mma_path<C::kTiles, C::kWarps, C::kStages>(P, part, smem, sh);
+  mma_path<C::kTiles, C::kWarps, C::kStages, C::kSpare>(P, part, smem, sh);
   pdl_launch_dependents();
 }
 
@@ -226,7 +227,7 @@ int launch(Kv4Params& P, int engine, double most, int sms, cudaStream_t stream) 
     rc = launch_one(kv4_verify_mma_kernel<R8>, P, dim3(sms), C::kWarps * 32, C::Mma::kSmem, stream);
   }
   if (rc != SPECATTN_OK) return rc;
-  return launch_one(kv4_join_kernel, P, dim3(P.n_units + 1, R8), 256, 0, stream);
+  return launch_one(kv4_join_kernel, P, dim3(P.n_units + 1, C::kSpare ? 1 : R8), 256, 0, stream);
 }
 
 }  // namespace
@@ -307,7 +308,8 @@ extern "C" int specattn_kv4_verify(const specattn_kv4_verify_args* args, void* c
   const int engine = A.flags & SPECATTN_VERIFY_ENGINE_TCGEN05 ? 2 : A.flags & SPECATTN_VERIFY_ENGINE_MMA_SYNC ? 1 : 0;
   const double longest = A.dense ? static_cast<double>(cache.block_table_stride) * cache.page_size : static_cast<double>(A.idx_stride);
   const double most = static_cast<double>(A.batch) * A.n_kv_heads * ((longest + A.tail_len) / kChunk + 1);
-  switch (r8) {
+  switch (P.rows <= 4 ? 0 : r8) {
+    case 0: return launch<0>(P, engine, most, sms, stream);
     case 1: return launch<1>(P, engine, most, sms, stream);
     case 2: return launch<2>(P, engine, most, sms, stream);
     case 3: return launch<3>(P, engine, most, sms, stream);

@@ -50,6 +50,13 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   const __half2 v = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&v);
 }
+// Two numbers as sums of two fp16 numbers each, off by 2^-21 of themselves or 2^-24, whichever is more: their first 11 bits, and
+// the rest, rounded.  (Cut, not rounded: a mask takes the place of a conversion back; 8 x 32768, 40 rows on tcgen05
+// 179 against 171 us, 24 on mma.sync 142 against 138.)
+__device__ __forceinline__ uint2 halves_f16(float lo, float hi) {
+  const float lo11 = __uint_as_float(__float_as_uint(lo) & 0xffffe000u), hi11 = __uint_as_float(__float_as_uint(hi) & 0xffffe000u);
+  return make_uint2(pack_f16(lo11, hi11), pack_f16(lo - lo11, hi - hi11));
+}
 __device__ __forceinline__ float2 widen16(uint32_t pair, int half) { return half ? widen<true>(pair) : widen<false>(pair); }
 __device__ __forceinline__ void cp_async4(uint32_t dst, const void* src, int bytes) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");

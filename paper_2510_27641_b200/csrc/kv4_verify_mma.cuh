@@ -6,9 +6,8 @@
 // agree, so a lane reads 16 bytes of a K row and 8 bytes of a V row as they lie in the cache.  Probabilities change
 // from result to operand layout by movmatrix.
 //
-// The middle of the codes is taken off by one more matrix instruction with a constant operand.  And every second tile of
-// positions uses 15 - e, the complement of the packed bits, with -w:
-//     sum w e = sum_even w e + sum_odd (-w) (15 - e) + 15 sum_odd w.
+// Every second tile of positions uses 15 - e, the complement of the packed bits, with -w:
+//     sum_i p_i V_i = sum_even w e + sum_odd (-w) (15 - e) + sum_even p y + sum_odd p (y + 15 t).
 // The accumulators then stay near zero instead of growing with sum w, and what the matrix units cut off at each step
 // stays as small (131072 positions: the output's error falls from 1.6 times that of its rounding to bf16 to no more
 // than it).
@@ -49,11 +48,15 @@ struct MmaShared {
   int limit[kQueries];   // how many tail positions a query row sees
 };
 
-template <int NT, int NWARP, int STAGES>
+// kSpare: a call of up to four query rows, whose weights' remainders take the columns of the four that there are not (those of
+// query q column 4 + q), and no instructions of their own.
+template <int NT, int NWARP, int STAGES, bool kSpare>
 __device__ __forceinline__ void mma_path(const Kv4Params& P, const Partition& part, unsigned char* smem, MmaShared<NT * 8>& S) {
   using K = MmaPath<NT, NWARP, STAGES>;
   const int tid = threadIdx.x, lane = tid & 31, warp = uniform(tid >> 5);
   const int g = lane >> 2, t = lane & 3;
+  static_assert(!kSpare || NT == 1, "four columns to spare");
+  const bool rests = kSpare && t >= 2;  // whose columns of the output are sums of remainders
   const uint32_t ring_at = smem_u32(smem + K::kQBytes + warp * K::kRing);
   const Units units = units_of(P);
   const int last = uniform(part.last);
@@ -121,14 +124,13 @@ __device__ __forceinline__ void mma_path(const Kv4Params& P, const Partition& pa
     });
     __syncthreads();
     const float k_mul = P.scale * 16777216.f * __int_as_float((127 - qexp) << 23);  // codes are c 2^-24 in the product
-    Two sq[NT], m[NT], l[NT], y[NT];  // of two queries: sum q; minus the running maximum (log2), sum of p, sum of p (y + 8 t)
-    float acc[8][NT][4], acc8[NT][4];                // output by (element tile, query tile), less its middle
+    Two sq[NT], m[NT], l[NT], y[NT];  // of two queries: sum q; minus the running maximum (log2), sum of p, sum of p (y + 0 or 15 t)
+    float acc[8][NT][4];                             // output by (element tile, query tile), less what y has
     float up = 3e38f;                                // the weights' power of two: w = p t up
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        acc8[nt][e] = 0.f;
 #pragma unroll
         for (int mt = 0; mt < 8; ++mt) acc[mt][nt][e] = 0.f;
       }
@@ -195,7 +197,7 @@ __device__ __forceinline__ void mma_path(const Kv4Params& P, const Partition& pa
           for (int r = 0; r < 2; ++r) {
             const float ks = kp[r].x * k_mul;
             t_of[r] = vp[r].x;
-            y_of[r] = fmaf(8.f, vp[r].x, vp[r].y);
+            y_of[r] = h2 ? fmaf(15.f, vp[r].x, vp[r].y) : vp[r].y;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
               const float2 x2 = each(fma2(two(s[nt][2 * r], s[nt][2 * r + 1]), two(ks, ks), fma2(two(kp[r].y, kp[r].y), sq[nt], m[nt])));
@@ -256,10 +258,15 @@ __device__ __forceinline__ void mma_path(const Kv4Params& P, const Partition& pa
             l[nt] = mul2(l[nt], two(f[0], f[1]));
             y[nt] = mul2(y[nt], two(f[0], f[1]));
 #pragma unroll
-            for (int e = 0; e < 2; ++e) f[e] *= scale_now;
+            for (int e = 0; e < 2; ++e) {
+              f[e] *= scale_now;
+              if (kSpare) {
+                const float of_query = __shfl_xor_sync(0xffffffffu, f[e], 2);
+                if (rests) f[e] = of_query;
+              }
+            }
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              acc8[nt][e] *= f[e & 1];
 #pragma unroll
               for (int mt = 0; mt < 8; ++mt) acc[mt][nt][e] *= f[e & 1];
             }
@@ -267,7 +274,7 @@ __device__ __forceinline__ void mma_path(const Kv4Params& P, const Partition& pa
         }
 
         // weights, and the second product
-        uint32_t pb[NT][2];
+        uint32_t pb[NT][2], pr[NT][2];  // in two halves: rounded to fp16, and what that leaves
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
           const float w_of = h2 ? -t_of[r] * up : t_of[r] * up;
@@ -277,16 +284,20 @@ __device__ __forceinline__ void mma_path(const Kv4Params& P, const Partition& pa
             l[nt] = add2(l[nt], p);
             y[nt] = fma2(p, two(y_of[r], y_of[r]), y[nt]);
             const float2 w = each(mul2(p, two(w_of, w_of)));
-            pb[nt][r] = transpose8(pack_f16(w.x, w.y));
+            uint2 halves = halves_f16(w.x, w.y);
+            if (kSpare) {
+              const uint32_t of_query = __shfl_xor_sync(0xffffffffu, halves.y, 2);
+              if (rests) halves.x = of_query;
+            } else {
+              pr[nt][r] = transpose8(halves.y);
+            }
+            pb[nt][r] = transpose8(halves.x);
           }
         }
         // V rows of positions 2 t, 2 t + 1, 2 t + 8, 2 t + 9 of the tile, 8 bytes to a lane
         const uint32_t v_row = stage + (kChunk + h2 * 16 + t) * kKv4Row + ((g * 8) ^ ((t & 2) << 4));
         const uint2 v[4] = {lds64(v_row), lds64(v_row + 4 * kKv4Row), lds64(v_row + 8 * kKv4Row), lds64(v_row + 12 * kKv4Row)};
         const uint32_t flip = h2 ? 0xffffffffu : 0u;
-        const uint32_t mid = h2 ? 0x80078007u : 0x80088008u;  // -7 (of -w: 15 w - 8 w), -8
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) mma_f16(acc8[nt], mid, mid, mid, mid, pb[nt][0], pb[nt][1]);
 #pragma unroll
         for (int w = 0; w < 2; ++w)
 #pragma unroll
@@ -302,6 +313,10 @@ __device__ __forceinline__ void mma_path(const Kv4Params& P, const Partition& pa
                              a3 = (z1 ^ flip) & 0x00f000f0u;
 #pragma unroll
               for (int nt = 0; nt < NT; ++nt) mma_f16(acc[mt][nt], a0, a1, a2, a3, pb[nt][0], pb[nt][1]);
+              if (!kSpare) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) mma_f16(acc[mt][nt], a0, a1, a2, a3, pr[nt][0], pr[nt][1]);
+              }
             }
           }
       }
@@ -312,6 +327,12 @@ __device__ __forceinline__ void mma_path(const Kv4Params& P, const Partition& pa
     // ---- the warps' parts meet ----
     float* meet = reinterpret_cast<float*>(smem + K::kQBytes);
     {
+      if (kSpare) {  // (the other columns' records are nobody's)
+#pragma unroll
+        for (int mt = 0; mt < 8; ++mt)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[mt][0][e] += __shfl_xor_sync(0xffffffffu, acc[mt][0][e], 2);
+      }
       const float down = 1.f / up;  // (0 where the warp has seen nothing: its sums are 0)
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
@@ -325,15 +346,14 @@ __device__ __forceinline__ void mma_path(const Kv4Params& P, const Partition& pa
           }
           float* rec = meet + (warp * K::kQueries + nt * 8 + 2 * t + e) * kRowFloats;
           if (g == 0) rec[kKv4D] = ls == 0.f ? -FLT_MAX : -(e ? each(m[nt]).y : each(m[nt]).x), rec[kKv4D + 1] = ls;
-          const float mid = acc8[nt][e];
           // lane g has elements 16 g ... 16 g + 15: tile mt holds 2 mt (codes in the low half of a byte) and 2 mt + 1
 #pragma unroll
           for (int mt = 0; mt < 8; mt += 2) {
             float4 o4;
-            o4.x = fmaf((acc[mt][nt][e] + mid) * 16777216.f, down, ys);
-            o4.y = fmaf(fmaf(acc[mt][nt][2 + e], 1048576.f, mid * 16777216.f), down, ys);
-            o4.z = fmaf((acc[mt + 1][nt][e] + mid) * 16777216.f, down, ys);
-            o4.w = fmaf(fmaf(acc[mt + 1][nt][2 + e], 1048576.f, mid * 16777216.f), down, ys);
+            o4.x = fmaf(acc[mt][nt][e] * 16777216.f, down, ys);
+            o4.y = fmaf(acc[mt][nt][2 + e] * 1048576.f, down, ys);
+            o4.z = fmaf(acc[mt + 1][nt][e] * 16777216.f, down, ys);
+            o4.w = fmaf(acc[mt + 1][nt][2 + e] * 1048576.f, down, ys);
             *reinterpret_cast<float4*>(rec + 16 * g + 2 * mt) = o4;
           }
         }

@@ -5,22 +5,22 @@
 // transposed, with 128 positions (or the 128 elements of an output row) as the M side and the N = 48 query rows (40 and
 // zeros) as the other:
 //     S^T [128 positions x N] = C_K [128 x 128] Q^T            C_K in tensor memory, Q in shared memory
-//     O^T [128 elements x N] += (C_V - 8)^T [128 x 128] W      both in shared memory, position-major
+//     O^T [128 elements x 80] += (C_V - 8)^T [128 x 128] W     both in shared memory, position-major; 40 columns of the weights'
+//                                                              first halves, 40 of their second: V is read once for both
 // Two threads own a position, each half of its codes and half of the queries: they unpack the K row's codes by masks (the
 // subnormals of fp16, see kv4_verify.cu) straight into their lane of tensor memory, and the V row's into a row of the
 // swizzled operand; they get the position's scores back as that lane of S^T, so that scale and zero point are the
 // threads' own; and they write the position's row of W.
-// 8 is taken off the V codes by a packed subtraction, exact in fp16: the weights' rounding errors then multiply a
-// code's distance from the middle, and the accumulators do not grow with the sum of the weights.
+// 8 is taken off the V codes by a packed subtraction, exact in fp16: the accumulators do not grow with the sum of the weights.
 //
 // Two groups of eight warps take tiles of 128 positions in turn, each with operands, accumulators and a running maximum of
 // its own, and run a phase apart.  In a group's turn:
 //     scores of tile i from tensor memory | K of tile i + 1 into it | vote (may the maximum stay?) and S^T of i + 1 starts |
-//     V of tile i, copies of tile i + 3 asked for | weights of tile i | O^T of tile i starts
-// 40 rows over 8 x 8 x 32768 positions: 155 us, 1.9 TB/s.  A tile takes an SM about 2600 cycles, where HBM would take 757 and
-// shared memory (16 KB of copies written and read, 32 KB of V operand, W and Q) 940: what bounds it is the chain of
-// instructions, barriers and products in flight in a group's turn.  (Taking 8 off by one more product with a constant
-// operand instead: 137 to 141 us at 24 rows.)
+//     V of tile i, copies of tile i + 2 asked for | weights of tile i | O^T of tile i starts
+// 40 rows over 8 x 8 x 32768 positions: 172 us, 1.7 TB/s.  A tile takes an SM about 2900 cycles, where HBM would take 757 and
+// shared memory (16 KB of copies written and read, 32 KB of V operand, W and Q) about 1000: what bounds it is the chain of
+// instructions, barriers and products in flight in a group's turn.  (A product each for the weights' two parts instead
+// of one of 80 columns: 198 against 180 us.)
 #pragma once
 #include "kv4_verify.cuh"
 
@@ -29,9 +29,9 @@ namespace {
 
 constexpr int kTile = 128;
 constexpr int kTcWarps = 16;
-constexpr int kTcRing = 3;
+constexpr int kTcRing = 2;
 constexpr int kTcStage = kChunk * kKv4Row;  // half rows of K and V for 32 positions
-constexpr int kTcSmem = 2 * 32768 + 2 * 16384 + 16384 + kTcWarps * kTcRing * kTcStage + 1024;
+constexpr int kTcSmem = 2 * 32768 + 4 * 16384 + 16384 + kTcWarps * kTcRing * kTcStage + 1024;
 
 struct Tc4Shared {
   alignas(8) unsigned long long s_bar[2], o_bar[2];
@@ -137,12 +137,13 @@ __device__ __forceinline__ float of_four(const float* in, int lane, Op op) {
 
 template <int R8>
 __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& part, unsigned char* smem_raw, Tc4Shared& S) {
-  constexpr int R = R8 * 8, N = (R8 + 1) / 2 * 16, CR = R / 2;  // query rows; columns of the products; a thread's columns
+  constexpr int R = R8 * 8, CR = R / 2;                     // query rows; a thread's
+  constexpr int N = (R8 + 1) / 2 * 16, NO = 2 * R;         // columns of the first product; of the second: rounded weights, then their remainders
   const int tid = threadIdx.x, lane = tid & 31, warp = uniform(tid >> 5);
   // group; half of a row's codes and of the queries; quarter of a tile; position of a tile = lane of tensor memory
   const int g = warp >> 3, half = (warp >> 2) & 1, wq = warp & 3, key = wq * 32 + lane, col0 = half * CR;
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
-  const uint32_t v_at = smem_u32(smem) + g * 32768, w_at = smem_u32(smem) + 65536 + g * 16384, q_at = smem_u32(smem) + 98304;
+  const uint32_t v_at = smem_u32(smem) + g * 32768, w_at = smem_u32(smem) + 65536 + g * 32768, q_at = smem_u32(smem) + 131072;
   const uint32_t ring_at = q_at + 16384 + warp * kTcRing * kTcStage;
   const Units units = units_of(P);
 
@@ -159,14 +160,18 @@ __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& par
     mbar_fence_init();
     S.abort = 0;
   }
-  // (columns of W and rows of Q beyond the query rows stay zero)
-  for (int i = tid; i < (2 * 16384 + 16384) / 16; i += kTcWarps * 32) reinterpret_cast<uint4*>(smem + 65536)[i] = make_uint4(0u, 0u, 0u, 0u);
+  // (rows of Q beyond the query rows stay zero)
+  for (int i = tid; i < 16384 / 16; i += kTcWarps * 32) reinterpret_cast<uint4*>(smem + 131072)[i] = make_uint4(0u, 0u, 0u, 0u);
   tm_before();
   __syncthreads();
   tm_after();
-  const uint32_t tm_a = static_cast<uint32_t>(uniform(S.tmem)) + g * 192, tm_s = tm_a + 64, tm_o = tm_a + 128, mine = static_cast<uint32_t>(wq * 32) << 16;
+  const uint32_t tm_a = static_cast<uint32_t>(uniform(S.tmem)) + g * 256, tm_s = tm_a + 64, tm_o = tm_a + 128, mine = static_cast<uint32_t>(wq * 32) << 16;
   const uint64_t q_op = operand(q_at, 16, 1024), v_op = operand(v_at, kTile * 128, 1024), w_op = operand(w_at, 16384, 1024);
   const bool issues = (warp & 7) == 0;  // a warp of each group
+  // where this thread's position has its weight for a column (W: 64 columns to a row of 128 bytes, pieces swizzled)
+  auto weight_at = [&](int col) {
+    return w_at + (col >> 6) * 16384 + key * 128 + ((((col & 63) >> 3) ^ (key & 7)) << 4) + (col & 4) * 2;
+  };
   uint32_t s_turn = 0, o_turn = 0;  // completions of this group's products that have been waited for
   auto wait_for = [&](unsigned long long* bar, uint32_t turn) {
     if (!mbar_wait(bar, turn & 1u, &S.abort)) S.abort = 1;
@@ -176,8 +181,8 @@ __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& par
   const int last = uniform(part.last);
   int u = uniform(part.unit), u_start = uniform(part.start), turn = 0;
   int b = 0, h = 0, seg0 = 0, seg1 = 0, n_tiles = 0, n_mine = 0, n_list = 0;
-  int pos_next = 0, pg_next = -2, pos_then = 0;  // of this group's tile i + 3, of the one behind it
-  uint32_t par_at1 = ~0u, par_at2 = ~0u;           // where its scales lie: of tiles i + 1, i + 2
+  int pos_next = 0, pg_next = -2, pos_then = 0;  // of this group's tile i + 2, of the one behind it
+  uint32_t par_at = ~0u;                           // where its scales lie: of tile i + 1
   uint2 par;                                       // (s, z), (t, y) of this thread's position in the next tile
   auto index = [&](int i) { return (seg0 + g + 2 * i) * kTile + key; };  // in the unit, of this thread's position in the group's tile i
   auto position = [&](const Gather& G, int i) { return i < n_mine ? G.position(index(i)) : 0; };
@@ -220,16 +225,14 @@ __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& par
     for (int s = 0; s < kTcRing + 2; ++s) pos[s] = position(G, s);
 #pragma unroll
     for (int s = 0; s < kTcRing + 1; ++s) pg[s] = page(G, s, pos[s]);
-    par_at1 = par_at2 = ~0u;
+    par_at = ~0u;
     if (0 < n_mine) par = scales(G, fetch(G, 0, pos[0], pg[0]));
     cp_commit();
-    if (1 < n_mine) par_at1 = fetch(G, 1, pos[1], pg[1]);
+    if (1 < n_mine) par_at = fetch(G, 1, pos[1], pg[1]);
     cp_commit();
-    if (2 < n_mine) par_at2 = fetch(G, 2, pos[2], pg[2]);
-    cp_commit();
-    pos_next = pos[3];
-    pg_next = pg[3];
-    pos_then = pos[4];
+    pos_next = pos[2];
+    pg_next = pg[2];
+    pos_then = pos[3];
   };
   const int start_at = uniform(part.first);
   if (start_at < last) begin(start_at);
@@ -297,7 +300,7 @@ __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& par
       const uint32_t stage = ring_at + (i % kTcRing) * kTcStage;
       const bool more = i + 1 < n_mine;
       const float2 kp = widen16(par.x, P.half), vp = widen16(par.y, P.half);
-      par = scales(G, par_at1);  // of the next tile
+      par = scales(G, par_at);  // of the next tile
       float x[CR];
       wait_for(&S.s_bar[g], s_turn++);
       tm_after();
@@ -364,10 +367,12 @@ __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& par
         }
 #pragma unroll
         for (int c = 0; c < CR; c += 4) {
-          float o[4], f[4], down[4];
+          float o[4], rest[4], f[4], down[4];
           if (i > 0) {
             tm_ld4(o, tm_o + mine + col0 + c);
+            tm_ld4(rest, tm_o + mine + R + col0 + c);
             tm_wait_ld4(o);
+            tm_pass4(rest);
           }
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
@@ -378,6 +383,7 @@ __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& par
             f[e] = i == 0 ? 0.f : ex2(-d);  // (the sums are still 0, and the first maximum may be far below it: no 0 inf)
             x[c + e] -= d;
             o[e] *= f[e] * scale_now;
+            rest[e] *= f[e] * scale_now;
             down[e] = d;
           }
 #pragma unroll
@@ -390,7 +396,7 @@ __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& par
               of.w -= down[e + 1];
             }
           }
-          if (i > 0) tm_st4(tm_o + mine + col0 + c, o);
+          if (i > 0) tm_st4(tm_o + mine + col0 + c, o), tm_st4(tm_o + mine + R + col0 + c, rest);
         }
         tm_wait_st();
       }
@@ -414,8 +420,7 @@ __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& par
         }
       }
       __syncwarp();  // the stage has been read
-      par_at1 = par_at2;
-      par_at2 = i + kTcRing < n_mine ? fetch(G, i + kTcRing, pos_next, pg_next) : ~0u;
+      par_at = i + kTcRing < n_mine ? fetch(G, i + kTcRing, pos_next, pg_next) : ~0u;
       cp_commit();
       pos_next = pos_then;
       pg_next = page(G, i + kTcRing + 1, pos_then);
@@ -424,17 +429,17 @@ __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& par
       const float w_of = t * up;
 #pragma unroll
       for (int c = 0; c < CR; c += 4) {
-        uint32_t w[2];
+        uint2 w[2];  // the halves of two each
 #pragma unroll
         for (int e = 0; e < 4; e += 2) {
           const Two p = two(ex2(x[c + e]), ex2(x[c + e + 1]));
           l[(c + e) / 2] = add2(l[(c + e) / 2], p);
           z[(c + e) / 2] = fma2(p, two(y8, y8), z[(c + e) / 2]);
           const float2 w2 = each(mul2(p, two(w_of, w_of)));
-          w[e / 2] = pack_f16(w2.x, w2.y);
+          w[e / 2] = halves_f16(w2.x, w2.y);
         }
-        const int r = col0 + c;
-        sts64(w_at + key * 128 + (((r >> 3) ^ (key & 7)) << 4) + (r & 4) * 2, w[0], w[1]);
+        sts64(weight_at(col0 + c), w[0].x, w[1].x);
+        sts64(weight_at(R + col0 + c), w[0].y, w[1].y);
       }
       fence_proxy_async();
       tm_before();
@@ -443,7 +448,7 @@ __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& par
         tm_after();
 #pragma unroll
         for (int kk = 0; kk < 8; ++kk)
-          mma_smem(tm_o, v_op + kk * 2048 / 16, w_op + kk * 2048 / 16, shape_word(N, 1), kk > 0 ? 1 : i);
+          mma_smem(tm_o, v_op + kk * 2048 / 16, w_op + kk * 2048 / 16, shape_word(NO, 1), kk > 0 ? 1 : i);
         mma_done(&S.o_bar[g]);
       }
       __syncwarp();
@@ -476,7 +481,7 @@ __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& par
     }
     __syncthreads();  // both groups are done with their operands: records take their place
     float* meet = reinterpret_cast<float*>(smem);
-    static_assert(R8 % 2 == 0 || 2 * R * kRowFloats * 4 <= 65536, "the spare columns of W have to stay zero");
+    static_assert(2 * R * kRowFloats * 4 <= 131072, "the spare rows of Q have to stay zero");
     if ((tid & 255) < R) {
       const int r = tid & 255;
       const float ls = (S.red[g][0][r][0] + S.red[g][1][r][0]) + (S.red[g][2][r][0] + S.red[g][3][r][0]);
@@ -492,15 +497,17 @@ __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& par
       const float down = (j & 2 ? 1048576.f : 16777216.f) / up;
 #pragma unroll
       for (int c = 0; c < CR; c += 4) {
-        float o[4];
+        float o[4], rest[4];
         if (this_mine > 0) {
           tm_ld4(o, tm_o + mine + col0 + c);
+          tm_ld4(rest, tm_o + mine + R + col0 + c);
           tm_wait_ld4(o);
+          tm_pass4(rest);
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int r = col0 + c + e;
-          meet[(g * R + r) * kRowFloats + d] = this_mine > 0 ? fmaf(o[e], down, S.sums[g][r]) : 0.f;
+          meet[(g * R + r) * kRowFloats + d] = this_mine > 0 ? fmaf(o[e] + rest[e], down, S.sums[g][r]) : 0.f;
         }
       }
     }
