@@ -508,10 +508,10 @@ int specattn_kv4_read(const specattn_kv4_rows_args* args, void* cuda_stream);
  * no negative stride, the codes of one head within 64 GB and its params within 16 GB of their first
  * (n_pages * stride_page + stride_kv + page_size * stride_slot).
  * flags: SPECATTN_VERIFY_ENGINE_MMA_SYNC or SPECATTN_VERIFY_ENGINE_TCGEN05 forces one of two implementations of the same
- * operation; TCGEN05 runs 33 to 40 query rows (SPECATTN_ERR_UNSUPPORTED otherwise).  With neither the library picks by the
- * sizes of the call: a caller of 33 to 40 rows whose lists are far shorter than idx_stride or the block
- * table (fewer than 1024 positions an SM in all) does better to force MMA_SYNC.  Results agree within the tolerance of the
- * operation either way.
+ * operation; TCGEN05 runs 25 to 48 query rows (SPECATTN_ERR_UNSUPPORTED otherwise).  With neither the library picks by the
+ * sizes of the call: MMA_SYNC for lists, and where dense for block tables with little room.  A caller of 33 rows or more whose lists
+ * hold well over 1024 positions an SM in all does better to force TCGEN05, one whose contexts are far shorter than the block table
+ * MMA_SYNC.  Results agree within the tolerance of the operation either way.
  * workspace: specattn_kv4_verify_workspace_bytes() bytes, 256-byte aligned, no preparation and no
  * state between calls; two calls that may overlap on the GPU need separate ones.
  * (The call signals programmatic launch completion early: it does not count as the launch in front of a

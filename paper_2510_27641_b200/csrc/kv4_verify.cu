@@ -13,7 +13,7 @@
 // of 138, 40 rows 155 instead of 172; the outputs were off by 1e-4 of their scale, fp16 ones by half as much again as their own
 // rounding.)
 //
-// Two paths compute this: on mma.sync (kv4_verify_mma.cuh) and, for 33 to 40 query rows, on tcgen05 (kv4_verify_tc.cuh).
+// Two paths compute this: on mma.sync (kv4_verify_mma.cuh) and, for 25 to 48 query rows, on tcgen05 (kv4_verify_tc.cuh).
 // Units (sequence, KV head) are cut on the device, where the lengths are; the parts meet through the workspace in a second
 // kernel, and nothing is held over from call to call.
 #include <cuda_runtime.h>
@@ -37,17 +37,26 @@ namespace {
 // What a call of R8 * 8 query rows runs with.
 //
 // mma.sync: as many warps as hold a warp's output in registers.  Two groups of query rows, which read a unit's rows twice,
-// from 33 rows on.  There tcgen05 takes 33 to 40 rows, from kTensorLeast chunks of 32 positions to an SM on that the call's
-// sizes (idx_stride, or the block table) leave room for: 8 sequences x 8 heads x 32768 positions with 40 rows are 172 us
-// against 260, x 2400 (33 chunks) 31.1 against 33.3, x 1200 25.0 against 22.9.  A kernel for each path: one for both, choosing by
-// the lengths it found, cost small calls 3 us and 10 to 17 where the instructions were not in L2.
-constexpr int kTensorLeast = 32;
+// from 33 rows on.
+//
+// tcgen05 takes 25 to 48 rows of calls over everything whose block table has room for least_chunks() chunks of 32 positions to an SM
+// or more.  8 sequences x 8 heads, mma.sync against tcgen05:
+//     x 32768   24 rows 138 / 143 us   28, 32 rows 174 / 152   40 rows 260 / 172   48 rows 261 / 200
+//     x 4800 (65 chunks)  34.1 / 36.1               41 / 38.5           55 / 43.8           55.5 / 49.6
+//     x 2400 (33 chunks)  23.6 / 25.8             27.8 / 27.6         33.4 / 31.3           33.5 / 35.5
+//     x 1200              18.0 / 20.6             20.8 / 21.7         23.0 / 25.0           23.1 / 28.5
+// (41 rows and more spill 200 bytes on tcgen05.)  Lists run on mma.sync, whatever room idx_stride gives them: their lengths are known
+// on the device only, and a selection's stride is the context, of which it keeps a few per cent (40 rows, 4 x 8 lists with room
+// for 131072: of 900 17.0 / 19.5 us, of 4000 32.0 / 32.2; only lists as long as 65536 lose, 252 / 166, and their caller may
+// say so).  A kernel for each path: one for both, choosing by the lengths it found, cost small calls 3 us and 10 to 17 where
+// the instructions were not in L2.
+constexpr int least_chunks(int r8) { return r8 == 6 ? 64 : 32; }
 template <int R8>  // (0: up to four rows)
 struct Config {
   static constexpr bool kSpare = R8 == 0;
   static constexpr int kGroups = R8 > 4 ? 2 : 1;               // of query rows, on mma.sync: 32 are as many as registers hold
   static constexpr int kTiles = kSpare ? 1 : (R8 + kGroups - 1) / kGroups;  // of eight queries
-  static constexpr bool kTensor = R8 == 5;
+  static constexpr bool kTensor = R8 >= 4 && R8 <= 6;
   static constexpr int kWarps = R8 <= 1 ? 16 : R8 == 2 ? 12 : 8;
   // Two chunks of 32 positions to a warp: one under way, one at work.  What the ring leaves is L1, where lists, tables and the
   // sectors of (s, z) pairs are met again (against three or four, with weights of 11 bits: 20 rows over 32 ragged lists 84
@@ -160,7 +169,7 @@ int validate(const specattn_kv4_verify_args* args) {
       static_cast<long long>(A.batch) * A.n_kv_heads > kMaxUnits)
     return SPECATTN_ERR_UNSUPPORTED;
   const int rows = A.n_q * (A.n_q_heads / A.n_kv_heads);
-  if ((A.flags & SPECATTN_VERIFY_ENGINE_TCGEN05) && (rows <= 32 || rows > 40)) return SPECATTN_ERR_UNSUPPORTED;
+  if ((A.flags & SPECATTN_VERIFY_ENGINE_TCGEN05) && (rows <= 24 || rows > 48)) return SPECATTN_ERR_UNSUPPORTED;
   return SPECATTN_OK;
 }
 
@@ -192,7 +201,7 @@ int launch_one(void (*kernel)(Kv4Params), const Kv4Params& P, dim3 grid, int thr
   return SPECATTN_OK;
 }
 
-// most: the largest number of chunks of 32 positions that the call can have, by its sizes
+// most: the largest number of chunks of 32 positions that a call over everything can have, by its sizes
 template <int R8>
 int launch(Kv4Params& P, int engine, double most, int sms, cudaStream_t stream) {
   using C = Config<R8>;
@@ -216,7 +225,7 @@ int launch(Kv4Params& P, int engine, double most, int sms, cudaStream_t stream) 
   P.rows_per_unit = C::kTiles * 8;
   int rc = SPECATTN_OK;
   if constexpr (C::kTensor) {
-    if (engine == 2 || (engine == 0 && most >= static_cast<double>(kTensorLeast) * sms)) {
+    if (engine == 2 || (engine == 0 && P.dense && most >= static_cast<double>(least_chunks(R8)) * sms)) {
       P.n_units = P.B * P.H;
       P.rows_per_unit = R8 * 8;
       rc = launch_one(kv4_verify_tc_kernel<R8>, P, dim3(sms), kTcWarps * 32, kTcSmem, stream);
@@ -306,7 +315,7 @@ extern "C" int specattn_kv4_verify(const specattn_kv4_verify_args* args, void* c
   P.test_lose = A.flags & SPECATTN_VERIFY_TEST_LOSE_ARRIVAL ? 1 : 0;
   const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
   const int engine = A.flags & SPECATTN_VERIFY_ENGINE_TCGEN05 ? 2 : A.flags & SPECATTN_VERIFY_ENGINE_MMA_SYNC ? 1 : 0;
-  const double longest = A.dense ? static_cast<double>(cache.block_table_stride) * cache.page_size : static_cast<double>(A.idx_stride);
+  const double longest = static_cast<double>(cache.block_table_stride) * cache.page_size;
   const double most = static_cast<double>(A.batch) * A.n_kv_heads * ((longest + A.tail_len) / kChunk + 1);
   switch (P.rows <= 4 ? 0 : r8) {
     case 0: return launch<0>(P, engine, most, sms, stream);

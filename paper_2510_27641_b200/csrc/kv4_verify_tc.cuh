@@ -1,9 +1,9 @@
-// The path of specattn_kv4_verify on tcgen05, for 33 to 40 query rows over long lists.
+// The path of specattn_kv4_verify on tcgen05, for 25 to 48 query rows.
 //
 // mma.sync does 1024 multiply-adds a cycle and SM, which 24 query rows use up at the speed of the memory; tcgen05 does
 // four times that, and its operands need not pass through registers.  As in the bf16 kernel both products are taken
-// transposed, with 128 positions (or the 128 elements of an output row) as the M side and the N = 48 query rows (40 and
-// zeros) as the other:
+// transposed, with 128 positions (or the 128 elements of an output row) as the M side and N = 48 query rows (40 and zeros,
+// say) as the other:
 //     S^T [128 positions x N] = C_K [128 x 128] Q^T            C_K in tensor memory, Q in shared memory
 //     O^T [128 elements x 80] += (C_V - 8)^T [128 x 128] W     both in shared memory, position-major; 40 columns of the weights'
 //                                                              first halves, 40 of their second: V is read once for both
