@@ -559,6 +559,11 @@ int specattn_kv4_verify(const specattn_kv4_verify_args* args, void* cuda_stream)
  * scores_out.  Other entries are left as they were.  Where a contributing probability is negative,
  * NaN or infinite the position gets its old value, undecayed, and row_status[u,b,g] (optional, cleared by
  * the call, for every u) SPECATTN_ROW_INVALID_PROB.
+ * Column i of a map is credited to slot i of the list.  Slots are tokens until specattn_evict's moves have been carried out; from then
+ * on slot i holds token positions[u,b,g,i], and a map (or a list of specattn_select_topp made from it) has to be in the order of
+ * the slots, too.  It is where the draft's own cache has been moved by the same lists (one list, or one for each of its KV heads,
+ * as in specattn_move_rows).  A draft that keeps its whole cache gives maps of tokens: the caller gathers them by positions
+ * before the call, each head's by the positions of the group that it feeds; nothing here can tell the one from the other.
  * Arrays, limits and alignment of draft_probs, kv_len and head_group as in specattn_select_topp (gamma at most
  * SPECATTN_MAX_ROWS_PER_LIST, batch and, where heads are grouped, batch * n_groups at most 65535);
  * scores are binary32 [n_layers, batch, n_groups, score_stride]. */
@@ -591,7 +596,8 @@ int specattn_accumulate(const specattn_accumulate_args* args, void* cuda_stream)
  *   Moves: the slots >= m that stay, ascending, go to the slots < m that do not, ascending:
  *   src[u,b,g,j] -> dst[u,b,g,j], j < n_moves[u,b,g] <= min(budget, L - budget).  Entries behind are
  *   left as they were.  No slot is both read and written, so moves may run in any order; rows in front
- *   that stay are not touched, and slots stop being in token order: positions tells it.
+ *   that stay are not touched, and slots stop being in token order: positions tells it.  (What the draft's maps and the lists made
+ *   from them then have to look like: see specattn_accumulate.)
  *   new_len[b] = m, which is the sequence's kv_len once the rows have been moved.
  *   scores_out (optional): the scores after the moves, 0 in slots [m, n) so that tokens appended there
  *   start from nothing; may equal scores.  positions_out (optional, needs positions): likewise, slots

@@ -183,7 +183,8 @@ def kv4_verify(q: torch.Tensor, codes: torch.Tensor, params: torch.Tensor, kv_le
                status: torch.Tensor | None = None, workspace: torch.Tensor | None = None, flags: int = 0, stream=None):
     """specattn_kv4_verify for one target layer: attention of q [B, T, H_q, 128] (of the type of ``params``) over the listed
     positions (idx [B, n_groups, stride], counts [B, n_groups]; all positions where ``dense``) and the tail of a 4-bit
-    cache.  Returns (out [B, T, H_q, 128] of q's type, or float32 where ``out`` is, lse f32 [B, T, H_q], status)."""
+    cache.  Returns (out [B, T, H_q, 128] of q's type, or float32 where ``out`` is, lse f32 [B, T, H_q], status).
+    A step over such a cache is select_topp and one call per target layer; VerifyStep and verify_step_host take 16-bit pools."""
     index = _device(q, codes, params, kv_len, block_table, None if dense else idx, None if dense else counts, out, lse, status, workspace)
     assert dense or (idx is not None and counts is not None), "idx and counts expected, or dense"
     shape = q.shape
@@ -247,7 +248,10 @@ def accumulate_attention(draft_probs: Sequence[torch.Tensor | None], kv_len: tor
                          out: torch.Tensor | None = None, row_status: torch.Tensor | None = None, stream=None):
     """specattn_accumulate: out = decay * scores + the attention that each position got in ``draft_probs`` (per draft
     layer a float32 tensor [B, H_d, gamma, L_stride], or None to leave the layer's entries of out alone).  scores, out: float32
-    [n_layers, B, n_groups, L]; out None: in place; scores None: zeros.  Returns (out, row_status)."""
+    [n_layers, B, n_groups, L]; out None: in place; scores None: zeros.  Returns (out, row_status).
+
+    Column i counts for slot i.  After an eviction slots are no longer tokens in order: the maps of a draft that keeps its whole
+    cache are first gathered by ``positions``, each head's by those of the group that it feeds."""
     n = len(draft_probs)
     probs = next((t for t in draft_probs if t is not None), None)
     assert probs is not None, "draft_probs: a layer's at least"
