@@ -2,15 +2,15 @@
 //
 // The mathematics.  With K_i = s_i c_i + z_i and V_i = t_i e_i + y_i (codes c, e in 0..15),
 //     q . K_i   = s_i (q . c_i) + z_i sum q
-//     sum_i p_i V_i = sum_i (p_i t_i) (e_i - 8) + sum_i p_i (y_i + 8 t_i)
-// so both products run over the codes themselves and the scales enter per (position, query) in binary32.  A code c
-// as the bit pattern of an fp16 number is the subnormal c 2^-24, and 16 c is c 2^-20: masking a word of packed codes
-// with 0x000f000f or 0x00f000f0 gives a register of two exact fp16 values and no conversion takes place (five
-// instructions for eight codes; tensor cores take subnormals as they are).  Queries are scaled by a power of two so
+//     sum_i p_i V_i = sum_i (p_i t_i) (e_i - m) + sum_i p_i (y_i + m t_i)
+// so both products run over the codes themselves (less an m that keeps the second's sums near zero) and the scales enter
+// per (position, query) in binary32.  A code c as the bit pattern of an fp16 number is the subnormal c 2^-24, and 16 c is
+// c 2^-20: masking a word of packed codes with 0x000f000f or 0x00f000f0 gives a register of two exact fp16 values and no
+// conversion takes place (five instructions for eight codes; tensor cores take subnormals as they are).  Queries are scaled by a power of two so
 // that they fit fp16 with all of their bits, those that meet the high codes of a byte by 2^-4 more.
 // fp16 holds 11 bits of a weight w = p t, and sums of outputs in binary32 should not depend on so few: a weight goes in as
 // two fp16 numbers, 21 bits, and the second product runs over both.  (With 11 bits alone 24 rows over 8 x 32768 took 122 us instead
-// of 138, 40 rows 155 instead of 172; the outputs were off by 1e-4 of their scale, fp16 ones by half as much again as their own
+// of 142, 40 rows 155 instead of 172; the outputs were off by 1e-4 of their scale, fp16 ones by half as much again as their own
 // rounding.)
 //
 // Two paths compute this: on mma.sync (kv4_verify_mma.cuh) and, for 25 to 48 query rows, on tcgen05 (kv4_verify_tc.cuh).
@@ -41,16 +41,16 @@ namespace {
 //
 // tcgen05 takes 25 to 48 rows of calls over everything whose block table has room for least_chunks() chunks of 32 positions to an SM
 // or more.  8 sequences x 8 heads, mma.sync against tcgen05:
-//     x 32768   24 rows 138 / 143 us   28, 32 rows 174 / 152   40 rows 260 / 172   48 rows 261 / 200
-//     x 4800 (65 chunks)  34.1 / 36.1               41 / 38.5           55 / 43.8           55.5 / 49.6
-//     x 2400 (33 chunks)  23.6 / 25.8             27.8 / 27.6         33.4 / 31.3           33.5 / 35.5
-//     x 1200              18.0 / 20.6             20.8 / 21.7         23.0 / 25.0           23.1 / 28.5
+//     x 32768   24 rows 142 / 143 us   28, 32 rows 170 / 155   40 rows 270 / 172   48 rows 270 / 199
+//     x 4800 (65 chunks)  33.6 / 36.0             40.0 / 38.9         54.8 / 43.8           55.4 / 49.6
+//     x 2400 (33 chunks)  23.0 / 25.7             27.0 / 27.6         33.3 / 31.5           33.3 / 35.5
+//     x 1200              17.6 / 20.4             20.6 / 21.8         22.6 / 24.9           22.9 / 28.4
 // (41 rows and more spill 200 bytes on tcgen05.)  Lists run on mma.sync, whatever room idx_stride gives them: their lengths are known
 // on the device only, and a selection's stride is the context, of which it keeps a few per cent (40 rows, 4 x 8 lists with room
-// for 131072: of 900 17.0 / 19.5 us, of 4000 32.0 / 32.2; only lists as long as 65536 lose, 252 / 166, and their caller may
+// for 131072: of 900 16.7 / 19.6 us, of 4000 32.4 / 32.7; only lists as long as 65536 lose, 256 / 167, and their caller may
 // say so).  A kernel for each path: one for both, choosing by the lengths it found, cost small calls 3 us and 10 to 17 where
 // the instructions were not in L2.
-constexpr int least_chunks(int r8) { return r8 == 6 ? 64 : 32; }
+constexpr int least_chunks(int r8) { return r8 == 5 ? 32 : 64; }
 template <int R8>  // (0: up to four rows)
 struct Config {
   static constexpr bool kSpare = R8 == 0;

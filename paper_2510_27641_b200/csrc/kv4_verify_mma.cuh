@@ -6,11 +6,10 @@
 // agree, so a lane reads 16 bytes of a K row and 8 bytes of a V row as they lie in the cache.  Probabilities change
 // from result to operand layout by movmatrix.
 //
-// Every second tile of positions uses 15 - e, the complement of the packed bits, with -w:
-//     sum_i p_i V_i = sum_even w e + sum_odd (-w) (15 - e) + sum_even p y + sum_odd p (y + 15 t).
-// The accumulators then stay near zero instead of growing with sum w, and what the matrix units cut off at each step
-// stays as small (131072 positions: the output's error falls from 1.6 times that of its rounding to bf16 to no more
-// than it).
+// The second eight positions of a tile use 15 - e, the complement of the packed bits, with -w:
+//     sum_i p_i V_i = sum_first w e + sum_second (-w) (15 - e) + sum_first p y + sum_second p (y + 15 t).
+// What an instruction adds is then around zero, and so are the accumulators, instead of growing with sum w: the matrix units cut
+// off towards zero as they add, and a sum of one sign loses a little every time.
 //
 // A warp owns chunks of 32 positions from the gather to the running maximum, sum and output, with a ring of its own
 // that cp.async fills: no barrier in the loop.  Warps meet at the end of a unit (sequence, KV head).
@@ -197,7 +196,7 @@ __device__ __forceinline__ void mma_path(const Kv4Params& P, const Partition& pa
           for (int r = 0; r < 2; ++r) {
             const float ks = kp[r].x * k_mul;
             t_of[r] = vp[r].x;
-            y_of[r] = h2 ? fmaf(15.f, vp[r].x, vp[r].y) : vp[r].y;
+            y_of[r] = r ? fmaf(15.f, vp[r].x, vp[r].y) : vp[r].y;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
               const float2 x2 = each(fma2(two(s[nt][2 * r], s[nt][2 * r + 1]), two(ks, ks), fma2(two(kp[r].y, kp[r].y), sq[nt], m[nt])));
@@ -277,7 +276,7 @@ __device__ __forceinline__ void mma_path(const Kv4Params& P, const Partition& pa
         uint32_t pb[NT][2], pr[NT][2];  // in two halves: rounded to fp16, and what that leaves
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-          const float w_of = h2 ? -t_of[r] * up : t_of[r] * up;
+          const float w_of = r ? -t_of[r] * up : t_of[r] * up;
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
             const Two p = two(ex2(s[nt][2 * r]), ex2(s[nt][2 * r + 1]));
@@ -297,7 +296,6 @@ __device__ __forceinline__ void mma_path(const Kv4Params& P, const Partition& pa
         // V rows of positions 2 t, 2 t + 1, 2 t + 8, 2 t + 9 of the tile, 8 bytes to a lane
         const uint32_t v_row = stage + (kChunk + h2 * 16 + t) * kKv4Row + ((g * 8) ^ ((t & 2) << 4));
         const uint2 v[4] = {lds64(v_row), lds64(v_row + 4 * kKv4Row), lds64(v_row + 8 * kKv4Row), lds64(v_row + 12 * kKv4Row)};
-        const uint32_t flip = h2 ? 0xffffffffu : 0u;
 #pragma unroll
         for (int w = 0; w < 2; ++w)
 #pragma unroll
@@ -309,8 +307,7 @@ __device__ __forceinline__ void mma_path(const Kv4Params& P, const Partition& pa
             for (int hi = 0; hi < 2; ++hi) {
               const int mt = w * 4 + half * 2 + hi;
               const uint32_t z0 = hi ? x0 >> 8 : x0, z1 = hi ? x1 >> 8 : x1;
-              const uint32_t a0 = (z0 ^ flip) & 0x000f000fu, a1 = (z0 ^ flip) & 0x00f000f0u, a2 = (z1 ^ flip) & 0x000f000fu,
-                             a3 = (z1 ^ flip) & 0x00f000f0u;
+              const uint32_t a0 = z0 & 0x000f000fu, a1 = z0 & 0x00f000f0u, a2 = ~z1 & 0x000f000fu, a3 = ~z1 & 0x00f000f0u;
 #pragma unroll
               for (int nt = 0; nt < NT; ++nt) mma_f16(acc[mt][nt], a0, a1, a2, a3, pb[nt][0], pb[nt][1]);
               if (!kSpare) {

@@ -5,13 +5,15 @@
 // transposed, with 128 positions (or the 128 elements of an output row) as the M side and N = 48 query rows (40 and zeros,
 // say) as the other:
 //     S^T [128 positions x N] = C_K [128 x 128] Q^T            C_K in tensor memory, Q in shared memory
-//     O^T [128 elements x 80] += (C_V - 8)^T [128 x 128] W     both in shared memory, position-major; 40 columns of the weights'
+//     O^T [128 elements x 80] += (C_V - m)^T [128 x 128] W     both in shared memory, position-major; 40 columns of the weights'
 //                                                              first halves, 40 of their second: V is read once for both
 // Two threads own a position, each half of its codes and half of the queries: they unpack the K row's codes by masks (the
 // subnormals of fp16, see kv4_verify.cu) straight into their lane of tensor memory, and the V row's into a row of the
 // swizzled operand; they get the position's scores back as that lane of S^T, so that scale and zero point are the
 // threads' own; and they write the position's row of W.
-// 8 is taken off the V codes by a packed subtraction, exact in fp16: the accumulators do not grow with the sum of the weights.
+// m, 8 and 7 in turn, tile by tile, is taken off the V codes by a packed subtraction, exact in fp16: the accumulators stay near zero
+// instead of growing with the sum of the weights.  (The units cut off towards zero as they add; with 8 alone, half a code from the
+// middle, 131072 positions came out 1.2e-4 of their size too large.)
 //
 // Two groups of eight warps take tiles of 128 positions in turn, each with operands, accumulators and a running maximum of
 // its own, and run a phase apart.  In a group's turn:
@@ -38,7 +40,7 @@ struct Tc4Shared {
   alignas(16) float4 base[2][32];  // of two of a group's queries: sums q, minus the running maxima
   float red[2][4][64][2];          // what the warps of a group reduce
   float t_red[2][4];
-  float sums[2][64];  // sum of p (y + 8 t)
+  float sums[2][64];  // sum of p (y + m t)
   float qsum[64];
   int limit[64];
   int bad[2], qmax[2];  // of this segment, and cleared for the next
@@ -254,7 +256,7 @@ __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& par
     }
     const float k_mul = P.scale * 16777216.f * __int_as_float((127 - query_exponent(S.qmax[turn])) << 23);
     const Gather G(P, b, h);
-    Two l[CR / 2], z[CR / 2];  // of two queries: sum of p, sum of p (y + 8 t) of this thread's positions
+    Two l[CR / 2], z[CR / 2];  // of two queries: sum of p, sum of p (y + m t) of this thread's positions
     float up = 3e38f;          // the weights' power of two: w = p t up
 #pragma unroll
     for (int r = 0; r < CR / 2; ++r) l[r] = z[r] = two(0.f, 0.f);
@@ -316,7 +318,7 @@ __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& par
       for (int c = 4; c < CR; c += 4) tm_pass4(x + c);
       // scores from the running maximum on
       const float ks = kp.x * k_mul;
-      float t = vp.x, y8 = fmaf(8.f, vp.x, vp.y), top = -INFINITY;
+      float t = vp.x, y8 = fmaf(i & 1 ? 7.f : 8.f, vp.x, vp.y), top = -INFINITY;
       const float4* base = S.base[g] + col0 / 2;
 #pragma unroll
       for (int r = 0; r < CR; r += 2) {
@@ -407,6 +409,7 @@ __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& par
       }
       {
         const uint32_t row = stage + (kChunk + lane) * 32, to = v_at + swizzled(key, 8 * half, kTile);
+        const uint32_t mid = i & 1 ? 0x00070007u : 0x00080008u;
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
           const uint4 raw = lds128(row + ((c << 4) ^ swap));
@@ -414,8 +417,8 @@ __device__ __forceinline__ void tc_path(const Kv4Params& P, const Partition& par
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             const uint32_t v = w[j] >> 8;
-            sts128(to ^ ((4 * c + j) << 4), minus(w[j] & 0x000f000fu, 0x00080008u),
-                   minus(w[j] & 0x00f000f0u, 0x00800080u), minus(v & 0x000f000fu, 0x00080008u), minus(v & 0x00f000f0u, 0x00800080u));
+            sts128(to ^ ((4 * c + j) << 4), minus(w[j] & 0x000f000fu, mid), minus(w[j] & 0x00f000f0u, mid << 4),
+                   minus(v & 0x000f000fu, mid), minus(v & 0x00f000f0u, mid << 4));
           }
         }
       }

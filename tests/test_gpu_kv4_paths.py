@@ -36,10 +36,10 @@ def test_lists_take_mma_sync_whatever_their_room(T, Hq):
     _check(few, tc[0][:, :2], tc[1][:, :2])
 
 
-@pytest.mark.parametrize("T,Hq,least", [(14, 4, False), (14, 4, True), (24, 4, False), (24, 4, True), (12, 4, False)])
+@pytest.mark.parametrize("T,Hq,least", [(14, 4, False), (14, 4, True), (20, 4, False), (20, 4, True), (24, 4, False), (24, 4, True), (12, 4, False)])
 def test_long_tables_take_tcgen05(T, Hq, least):
-    """28, 48 and 24 rows, at either side of the limit of 32 (or 64) chunks to an SM."""
-    limit = (32 if T == 14 else 64) * torch.cuda.get_device_properties(0).multi_processor_count
+    """28, 40, 48 and 24 rows, at either side of the limit of 64 (40 rows: 32) chunks to an SM."""
+    limit = (32 if T == 20 else 64) * torch.cuda.get_device_properties(0).multi_processor_count
     page = 32
     per_seq = limit // (2 * 2) + (1 if least else -2 if T != 12 else 5000)   # of two sequences' two heads; a chunk to a page
     c = _case(144, 2, T, Hq, 2, [40, 33], None, dense=True, page=page)

@@ -48,3 +48,42 @@ def test_a_query_of_nan_or_infinity_spoils_no_other_of_a_few(T, Hq, Hkv):
         assert torch.all(torch.isnan(out2[0, 0, 0]))
         out2[0, 0, 0], lse2[0, 0, 0] = out[0, 0, 0], lse[0, 0, 0]
         assert torch.equal(out2, out) and torch.equal(lse2, lse)
+
+
+@pytest.mark.parametrize("engine", ["mma.sync", "tcgen05"])
+def test_long_sums_are_held_as_well_as_the_16_bit_operators(engine):
+    """131072 positions, outputs in binary32, on the same engine of both operators and values of the same distribution.
+
+    Both add up the same number of products in the same units, which cut off towards zero; a sum whose terms have a mean
+    loses a part of it each time, one around zero gains as often as it loses.  Errors are root mean squares of the
+    output's; a code lies up to 15 steps from where its tile counts from and a weight comes in two parts: three times
+    the 16-bit operator's error."""
+    import paper_2510_27641_b200 as sa
+    gen = torch.Generator(device=DEV).manual_seed(119)
+    n, page, T, Hq, Hkv = 131072, 16, 5, 64, 8
+    grp = Hq // Hkv
+    x = torch.randn(2, n, Hkv, 128, generator=gen, device=DEV)
+    x[0] += torch.randn(128, generator=gen, device=DEV)
+    x[1] *= 0.5
+    x = x.to(torch.bfloat16)
+    codes, params = sa.kv4_cache(n // page, page, Hkv)
+    start, lens = torch.zeros(1, dtype=torch.int32, device=DEV), torch.tensor([n], dtype=torch.int32, device=DEV)
+    sa.kv4_append(x[0][None], x[1][None], codes, params, start, pages_per_seq=n // page)
+    pool = torch.stack(list(x), 0).view(2, n // page, page, Hkv, 128).transpose(0, 1).contiguous()
+    q = (1.5 * torch.randn(1, T, Hq, 128, generator=gen, device=DEV)).to(torch.bfloat16)
+    flags = {"mma.sync": sa.VERIFY_ENGINE_MMA_SYNC, "tcgen05": sa.VERIFY_ENGINE_TCGEN05}[engine]
+    kw = dict(pages_per_seq=n // page, dense=True, flags=flags)
+    out4, out16 = (torch.empty(1, T, Hq, 128, device=DEV) for _ in range(2))
+    sa.kv4_verify(q, codes, params, lens, out=out4, **kw)
+    sa.sparse_verify(q, pool, lens, out=out16, **kw)
+
+    def error(out, k, v):
+        want = torch.softmax(q[0, :, :grp].double() @ k.T / 128 ** 0.5, -1) @ v
+        return float((out[0, :, :grp].double() - want).norm() / want.norm())
+
+    def stands_for(side):   # of head 0
+        c, p = codes[:, side, :, 0].reshape(n, 64), params[:, side, :, 0].reshape(n, 2).double()
+        return torch.stack([c % 16, c // 16], -1).flatten(-2).double() * p[:, :1] + p[:, 1:]
+
+    e4, e16 = error(out4, stands_for(0), stands_for(1)), error(out16, x[0, :, 0].double(), x[1, :, 0].double())
+    assert e4 <= 3 * e16, (e4, e16)
