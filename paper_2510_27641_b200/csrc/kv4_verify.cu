@@ -10,8 +10,8 @@
 // that they fit fp16 with all of their bits, those that meet the high codes of a byte by 2^-4 more.
 // fp16 holds 11 bits of a weight w = p t, and sums of outputs in binary32 should not depend on so few: a weight goes in as
 // two fp16 numbers, 21 bits, and the second product runs over both.  (With 11 bits alone 24 rows over 8 x 32768 took 122 us instead
-// of 142, 40 rows 155 instead of 172; the outputs were off by 1e-4 of their scale, fp16 ones by half as much again as their own
-// rounding.)
+// of 142, 40 rows 155 instead of 172; the outputs were off by 1e-4 to 5e-4 of their size, fp16 ones by half as much again as
+// their own rounding.)
 //
 // Two paths compute this: on mma.sync (kv4_verify_mma.cuh) and, for 25 to 48 query rows, on tcgen05 (kv4_verify_tc.cuh).
 // Units (sequence, KV head) are cut on the device, where the lengths are; the parts meet through the workspace in a second
